@@ -1,0 +1,520 @@
+"""The 8-bit LM head and the sampling rules, as a serving program calls them.
+
+Four kinds of call:
+
+- ``logits``: the logits of N rows from an LM head held in 8-bit floating point (e4m3) with one
+  power-of-two scale for each block of 128 ids x 128 columns. The bf16 hidden states are quantised
+  within the call, one scale for each row and 128 columns.
+- ``verify``: one verification step of a batch of draft trees on the 8-bit or the bf16 LM head, with
+  or without sampling rules: penalties for repeated tokens, a bias and a grammar mask of each node.
+- ``adjust``: the same rules on logits in memory, for trees and for plain decoding.
+- ``counts``: the history table that the rules read, from the requests' token lists.
+
+Inputs: weights N(0, 0.02), hidden states N(0, 1) plus a multiple of the weight row of a likely token
+(a model's logits have a top token that stands out, most of the time), tokens with a skewed
+distribution, so that histories and drafts repeat some.
+"""
+
+import math
+import random
+
+import torch
+
+own = False
+
+LLAMA_V, QWEN_V, DRAFT_V, H8B = 128256, 151936, 32000, 4096
+PROMPT = 1 << 30        # history table: tokens of the prompt; the lower bits count generated ones
+F8 = torch.float8_e4m3fn
+BLOCK = 128
+
+
+def _logits(name, H, V, N, dtype):
+    return dict(name=name, op="logits", H=H, V=V, N=N, dtype=dtype)
+
+
+def _verify(name, head, H, V, B, N, rules):
+    return dict(name=name, op="verify", head=head, H=H, V=V, B=B, N=N, rules=rules)
+
+
+def _adjust(name, V, B, N, dtype, tree, mask):
+    return dict(name=name, op="adjust", V=V, B=B, N=N, dtype=dtype, tree=tree, mask=mask)
+
+
+def listed():
+    return [
+        # Next-token logits of one user: the weight is read once, latency counts.
+        _logits("logits_b1", H8B, LLAMA_V, 1, "float32"),
+        # A decoding batch of 57 users, bf16 logits for a sampler.
+        _logits("logits_b57_bf16", H8B, QWEN_V, 57, "bfloat16"),
+        # Rows of a few trees on an odd vocabulary and a hidden size that ends inside a block.
+        _logits("logits_odd", 2880, 40003, 333, "float32"),
+        # One user, a 60-node draft tree: the headline workload of bench.py on the 8-bit weight.
+        _verify("fp8_b1_tree60", "fp8", H8B, LLAMA_V, 1, 60, False),
+        # The matrix-product-bound batch: 32 users with 64 nodes each.
+        _verify("fp8_b32x64", "fp8", H8B, LLAMA_V, 32, 2048, False),
+        # Eight users with ragged trees, all rules.
+        _verify("fp8_rules_b8", "fp8", H8B, QWEN_V, 8, 378, True),
+        # One user with structured output on the bf16 weight.
+        _verify("bf16_rules_b1", "bf16", H8B, LLAMA_V, 1, 60, True),
+        # The smallest call: one user's next token on a 32000-id vocabulary.
+        _adjust("adjust_b1", DRAFT_V, 1, 1, "float32", False, True),
+        # Plain decoding of 64 users, bf16 logits, no grammar.
+        _adjust("adjust_b64_bf16", QWEN_V, 64, 64, "bfloat16", False, False),
+        # The logits of 32 draft trees, a grammar state for each node.
+        _adjust("adjust_tree_b32", LLAMA_V, 32, 2048, "float32", True, True),
+        # A short chat that joins the batch.
+        dict(name="counts_b1", op="counts", V=DRAFT_V, B=1, T=777),
+        # All histories of a full batch, up to about 14000 tokens each.
+        dict(name="counts_b64", op="counts", V=QWEN_V, B=64, T=524288),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _vocab(rng):
+    return rng.choice([DRAFT_V, LLAMA_V, QWEN_V, _log_int(rng, 1000, 152000)])
+
+
+def _requests(rng, N):
+    return max(1, min(64, N // rng.randint(3, 64)))
+
+
+def draw(rng):
+    op = rng.choice(["logits"] * 3 + ["verify"] * 4 + ["adjust"] * 3 + ["counts"])
+    if op == "logits":
+        return dict(op=op, H=64 * rng.randint(8, 80), V=_vocab(rng), N=_log_int(rng, 1, 500),
+                    dtype=rng.choice(["float32", "bfloat16", "float16"]))
+    if op == "verify":
+        H, V = 64 * rng.randint(8, 80), _vocab(rng)
+        N = min(_log_int(rng, 2, 2048), int(2048 * H8B * LLAMA_V / (H * V)))
+        return dict(op=op, head=rng.choice(["fp8", "fp8", "bf16"]), H=H, V=V, B=_requests(rng, N),
+                    N=N, rules=rng.random() < 0.6)
+    if op == "adjust":
+        V, tree = _vocab(rng), rng.random() < 0.6
+        N = min(_log_int(rng, 1, 2048), 2048 * LLAMA_V // V)
+        return dict(op=op, V=V, B=_requests(rng, N) if tree else N, N=N,
+                    dtype=rng.choice(["float32", "bfloat16", "float16"]), tree=tree,
+                    mask=rng.random() < 0.6)
+    B = _log_int(rng, 1, 64)
+    return dict(op=op, V=_vocab(rng), B=B, T=B * _log_int(rng, 4, 8192) + rng.randint(0, 3))
+
+
+# ---- inputs
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _rand(gen, shape):
+    return torch.rand(shape, generator=gen, device="cuda")
+
+
+def _normal(gen, shape, std, dtype=torch.bfloat16):
+    return torch.empty(shape, dtype=dtype, device="cuda").normal_(0.0, std, generator=gen)
+
+
+def _tokens(gen, n, V):
+    """n ids, the low ones more often."""
+    return (_rand(gen, (n,)).double().pow(3) * V).long().clamp(max=V - 1)
+
+
+def _shares(total, B, least, seed):
+    """Sizes of B parts of `total`, ragged, at least `least` each, the same for every seed."""
+    rng = random.Random(seed)
+    w = [rng.uniform(0.3, 1.7) for _ in range(B)]
+    n = [least + int((total - least * B) * x / sum(w)) for x in w]
+    for k in range(total - sum(n)):
+        n[k % B] += 1
+    return n
+
+
+def _offsets(n):
+    off = [0]
+    for k in n:
+        off.append(off[-1] + k)
+    return off
+
+
+def _trees(B, N, rng):
+    """(parent, offsets) of a packed batch: chains, and trees whose nodes hang under one of the four
+    nodes before them."""
+    parent, off = [], _offsets(_shares(N, B, 1, 1000003 * B + N))
+    for b, (lo, hi) in enumerate(zip(off, off[1:])):
+        chain = b % 3 == 0 and hi - lo <= 17
+        for c in range(hi - lo):
+            parent.append(-1 if c == 0 else lo + (c - 1 if chain else max(0, c - rng.randint(1, 4))))
+    return parent, off
+
+
+def _pow2_block_scale(amax):
+    """The biased exponent of the least power of two 2^k with amax <= 448 * 2^k, k >= -126."""
+    bits = amax.float().view(torch.int32)
+    return ((bits >> 23) - 8 + ((bits & 0x7FFFFF) > 0x600000)).clamp(min=1)
+
+
+def _pow2(e):
+    return (e.int() << 23).view(torch.float32)
+
+
+def _quantised_weight(w):
+    """A checkpoint's e4m3 weight [V][H] and its scales' exponents [ceil(V / 128)][ceil(H / 128)]."""
+    V, H = w.shape
+    KB = -(-H // BLOCK)
+    q, scale = torch.empty((V, H), dtype=F8, device="cuda"), []
+    for lo in range(0, V, 128 * BLOCK):
+        x = w[lo:lo + 128 * BLOCK].float()
+        n = -(-x.shape[0] // BLOCK)
+        pad = torch.zeros((n * BLOCK, KB * BLOCK), device="cuda")
+        pad[:x.shape[0], :H] = x
+        pad = pad.view(n, BLOCK, KB, BLOCK)
+        e = _pow2_block_scale(pad.abs().amax((1, 3)))
+        r = pad * _pow2(254 - e)[:, None, :, None]
+        q[lo:lo + 128 * BLOCK] = r.view(n * BLOCK, KB * BLOCK)[:x.shape[0], :H].to(F8)
+        scale.append(e.to(torch.uint8))
+    return q, torch.cat(scale)
+
+
+def _model(case, gen):
+    """The LM-head weight, hidden states and each row's likely token. Three rows in four have one
+    that stands out."""
+    H, V, N = case["H"], case["V"], case["N"]
+    w = _normal(gen, (V, H), 0.02)
+    likely = _tokens(gen, N, V)
+    pull = 4096 / H * (2.0 + 8.0 * _rand(gen, (N, 1))) * (_rand(gen, (N, 1)) < 0.75)
+    hidden = (_normal(gen, (N, H), 1.0, torch.float32) + pull * w[likely].float()).bfloat16()
+    return w, hidden, likely
+
+
+def _history(gen, B, V, n_tok):
+    """Table of B requests with n_tok tokens each, the first half of them the prompt's."""
+    table = torch.zeros((B, V), dtype=torch.int32, device="cuda")
+    row = torch.arange(B, device="cuda")[:, None]
+    gens, prompt = _tokens(gen, B * n_tok, V).view(B, n_tok), _tokens(gen, B * n_tok, V).view(B, n_tok)
+    table.view(-1).index_add_(0, (row * V + gens).view(-1),
+                              torch.ones(B * n_tok, dtype=torch.int32, device="cuda"))
+    table.view(-1)[(row * V + prompt).view(-1)] += PROMPT
+    return table
+
+
+def _rules(gen, B, N, V, mask):
+    s = dict(counts=_history(gen, B, V, 1000), repetition=1.0 + 0.3 * _rand(gen, (B,)),
+             presence=0.6 * _rand(gen, (B,)), frequency=0.4 * _rand(gen, (B,)))
+    u = _rand(gen, (B, V))
+    bias = torch.where(u < 200 / V, 4.0 * torch.randn((B, V), generator=gen, device="cuda"), 0.0)
+    bias.masked_fill_(u < 12 / V, -math.inf)                    # banned ids
+    s["bias"] = bias
+    s["allowed"] = None
+    if mask:
+        # a quarter of the nodes is unconstrained; the others allow an eighth of the ids or a few words
+        words = -(-V // 32)
+        bits = torch.randint(-2**31, 2**31, (3, N, words), generator=gen, device="cuda", dtype=torch.int64)
+        kind = torch.randint(0, 4, (N, 1), generator=gen, device="cuda")
+        m = bits[0] & bits[1] & bits[2]
+        m = torch.where(kind == 0, -1, torch.where(kind == 3, m * (_rand(gen, (N, words)) < 0.01), m))
+        if N >= 16:
+            m[N // 2] = 0                                       # a dead end of the grammar
+        s["allowed"] = m.to(torch.int32)
+    return s
+
+
+def _prepare_logits(case, seed):
+    gen = _gen(seed)
+    w, hidden, _ = _model(case, gen)
+    q, scale = _quantised_weight(w)
+    s = dict(op="logits", hidden=hidden, q=q, scale=scale, dtype=getattr(torch, case["dtype"]))
+    if own:
+        import paper_2609_02897_amd as asv
+        s["head"] = asv.pack_lm_head_fp8(q, scale)
+    return s
+
+
+def _prepare_verify(case, seed):
+    B, N, V, H = case["B"], case["N"], case["V"], case["H"]
+    rng, gen = random.Random(seed), _gen(seed)
+    w, hidden, likely = _model(case, gen)
+    parent, off = _trees(B, N, rng)
+    par = _i32(parent)
+    # a drafter that agrees about half of the time, and now and then repeats its parent's token
+    tok, other = likely[par.clamp(min=0).long()], _tokens(gen, N, V)
+    u = _rand(gen, (N,))
+    tok = torch.where(u < 0.6, tok, other)
+    tok = torch.where(u > 0.9, tok[par.clamp(min=0).long()], tok).to(torch.int32)
+    s = dict(op="verify", hidden=hidden, parent=par, off=_i32(off), tok=tok, V=V,
+             depth=_depth(parent), rules=None,
+             tau=torch.tensor([rng.choice([0.0, 0.05, 0.1, 0.2, 0.3]) for _ in range(B)], device="cuda"))
+    if case["head"] == "fp8":
+        s["q"], s["scale"] = _quantised_weight(w)
+    else:
+        s["w"] = w
+    if case["rules"]:
+        s["rules"] = _rules(gen, B, N, V, True)
+    if own:
+        import paper_2609_02897_amd as asv
+        s["head"] = asv.pack_lm_head_fp8(s["q"], s["scale"]) if case["head"] == "fp8" else asv.pack_lm_head(w)
+        s["out"] = asv.alloc_outputs(B, N, hidden.device, False)
+        s["out"].drafted_logit.zero_()          # the roots' entries are not written by the call
+        s["ws"] = asv.alloc_workspace(B, N, H, V, hidden.device, s["head"])
+    return s
+
+
+def _depth(parent):
+    d = []
+    for p in parent:
+        d.append(0 if p < 0 else d[p] + 1)
+    return max(d)
+
+
+def _prepare_adjust(case, seed):
+    B, N, V = case["B"], case["N"], case["V"]
+    rng, gen = random.Random(seed), _gen(seed)
+    dtype = getattr(torch, case["dtype"])
+    s = dict(op="adjust", logits=_normal(gen, (N, V), 2.5, torch.float32).to(dtype),
+             rules=_rules(gen, B, N, V, case["mask"]), off=None, parent=None, tok=None, depth=0)
+    if case["tree"]:
+        parent, off = _trees(B, N, rng)
+        s.update(off=_i32(off), parent=_i32(parent), tok=_tokens(gen, N, V).to(torch.int32),
+                 depth=_depth(parent))
+    s["out"] = torch.empty_like(s["logits"])
+    return s
+
+
+def _prepare_counts(case, seed):
+    B, T = case["B"], case["T"]
+    n = _shares(T, B, 1, 7919 * B + T)
+    rng = random.Random(seed)
+    return dict(op="counts", V=case["V"], tok=_tokens(_gen(seed), T, case["V"]).to(torch.int32),
+                off=_i32(_offsets(n)), prompt=_i32([rng.randint(0, k) for k in n]))
+
+
+def prepare(case, seed):
+    return {"logits": _prepare_logits, "verify": _prepare_verify, "adjust": _prepare_adjust,
+            "counts": _prepare_counts}[case["op"]](case, seed)
+
+
+# ---- the plain forms
+
+def _dequantised(q, e):
+    """e4m3 codes [R][H] times the scales 2^(e - 127) of their blocks, e [R or R / 128][H / 128]."""
+    R, H = q.shape
+    if e.shape[0] != R:
+        e = e[torch.arange(R, device=q.device) // BLOCK]
+    return q.float() * _pow2(e)[:, torch.arange(H, device=q.device) // BLOCK]
+
+
+def _quantised_rows(x):
+    """(codes, scale exponents) of bf16 rows, a scale for each 128 columns."""
+    N, H = x.shape
+    KB = -(-H // BLOCK)
+    pad = torch.zeros((N, KB * BLOCK), device=x.device)
+    pad[:, :H] = x.float()
+    e = _pow2_block_scale(pad.view(N, KB, BLOCK).abs().amax(2))
+    q = pad.view(N, KB, BLOCK) * _pow2(254 - e)[:, :, None]
+    return q.view(N, KB * BLOCK)[:, :H].to(F8), e
+
+
+def _head_logits(s):
+    if "w" in s:
+        return s["hidden"].float() @ s["w"].float().T
+    return _dequantised(*_quantised_rows(s["hidden"])) @ _dequantised(s["q"], s["scale"]).T
+
+
+def _request_of(off, N):
+    return torch.searchsorted(off[1:].contiguous(), torch.arange(N, device=off.device, dtype=off.dtype), right=True)
+
+
+def _ruled(z, rules, off, parent, tok, depth):
+    """The rules on float32 logits z [N][V]."""
+    N, V = z.shape
+    at = torch.arange(N, device=z.device)
+    req = at if off is None else _request_of(off, N)
+    c = rules["counts"][req]
+    if parent is not None:
+        node = at
+        for _ in range(depth):                  # the drafted tokens on each node's path
+            up = parent[node].long()
+            c.view(-1).index_add_(0, at * V + tok[node].long(), (up >= 0).to(torch.int32))
+            node = torch.where(up >= 0, up, node)
+    generated = (c & (PROMPT - 1)).float()
+    rep, pres, freq = (rules[k][req][:, None] for k in ("repetition", "presence", "frequency"))
+    z = torch.where(c != 0, torch.where(z > 0, z / rep, z * rep), z)
+    z = z - (generated > 0) * (pres + freq * generated) + rules["bias"][req]
+    if rules["allowed"] is not None:
+        v = torch.arange(V, device=z.device)
+        z = torch.where((rules["allowed"][:, v // 32] >> (v % 32)) & 1 != 0, z, -math.inf)
+    return z
+
+
+def _walked(s, z):
+    """The margin rule and the walk on logits z."""
+    par, off, tok = s["parent"].long(), s["off"].long(), s["tok"].long()
+    N, B = z.shape[0], off.shape[0] - 1
+    m, arg = z.max(1).values, z.argmax(1)
+    arg = torch.where(m > -math.inf, arg, -1)
+    root = par < 0
+    up = par.clamp(min=0)
+    g = torch.where(root, 0.0, z[up, tok])
+    tau = s["tau"][_request_of(s["off"], N)]
+    ok = (tok == arg[up]) | (tau == 0) | (g - m[up] >= tau.log())
+    ok = root | (ok & ((g > -math.inf) if s["rules"] is not None else True))
+    # each node's child of the highest drafted logit, the first of equal ones
+    top = torch.full((N,), -math.inf, device=z.device).scatter_reduce(0, up[~root], g[~root], "amax")
+    best = torch.full((N,), N, device=z.device).scatter_reduce(
+        0, up[~root], torch.where(g == top[up], torch.arange(N, device=z.device), N)[~root], "amin")
+    cur, length = off[:-1], torch.zeros(B, dtype=torch.int64, device=z.device)
+    path = torch.full((N + 1,), -1, dtype=torch.int64, device=z.device)
+    going = torch.ones(B, dtype=torch.bool, device=z.device)
+    for _ in range(s["depth"]):
+        nxt = best[cur]
+        going = going & (nxt < N) & ok[nxt.clamp(max=N - 1)]
+        path[torch.where(going, off[:-1] + length, N)] = nxt
+        length, cur = length + going, torch.where(going, nxt, cur)
+    return dict(row_max=m, row_lse=torch.logsumexp(z, 1), row_argmax=arg.int(), drafted_logit=g,
+                accept=ok.to(torch.uint8), accepted_len=length.int(), bonus_token=arg[cur].int(),
+                accepted_path=path[:N].int(), req_status=torch.zeros(B, dtype=torch.int32, device=z.device))
+
+
+def _plain(s):
+    if s["op"] == "logits":
+        return _head_logits(s).to(s["dtype"])
+    if s["op"] == "verify":
+        z = _head_logits(s)
+        if s["rules"] is not None:
+            z = _ruled(z, s["rules"], s["off"], s["parent"], s["tok"], s["depth"])
+        return _walked(s, z)
+    if s["op"] == "adjust":
+        return _ruled(s["logits"].float(), s["rules"], s["off"], s["parent"], s["tok"],
+                      s["depth"]).to(s["logits"].dtype)
+    T, B, V = s["tok"].shape[0], s["off"].shape[0] - 1, s["V"]
+    at = torch.arange(T, device="cuda")
+    req = _request_of(s["off"], T)
+    prompt = at - s["off"][req] < s["prompt"][req]
+    table = torch.zeros(B * V, dtype=torch.int32, device="cuda")
+    key = req * V + s["tok"]
+    table.index_add_(0, key, (~prompt).to(torch.int32))
+    seen = torch.zeros(B * V, dtype=torch.int32, device="cuda").index_add_(0, key, prompt.to(torch.int32))
+    return (table + (seen > 0) * PROMPT).view(B, V)
+
+
+# ---- one pass
+
+def run(s):
+    if not own:
+        return _plain(s)
+    import paper_2609_02897_amd as asv
+    if s["op"] == "logits":
+        return asv.lm_head_logits(s["hidden"], s["head"], dtype=s["dtype"])
+    if s["op"] == "counts":
+        return asv.token_counts(s["tok"], s["off"], s["V"], s["prompt"])[0]
+    rules = None if s["rules"] is None else asv.LogitRules(**s["rules"])
+    if s["op"] == "adjust":
+        return asv.adjust_logits(s["logits"], rules, s["off"], s["parent"], s["tok"], out=s["out"])
+    out = asv.verify(s["hidden"], s["head"], s["tok"], s["parent"], s["off"], s["tau"], rules=rules,
+                     out=s["out"], workspace=s["ws"])
+    return {f: getattr(out, f) for f in out._fields if f != "draft_conf"}
+
+
+# ---- what a pass cannot do without
+
+def work(case):
+    B, V = case["B"] if "B" in case else 0, case["V"]
+    if case["op"] == "counts":
+        return {"bytes": 4 * case["T"] + 8 * B + 4 * B * V, "flops": 0}
+    N = case["N"]
+    rules = 0
+    if case["op"] == "adjust" or case.get("rules"):
+        mask = case["op"] == "verify" or case["mask"]
+        rules = 8 * B * V + 12 * B + (4 * N * -(-V // 32) if mask else 0)
+    if case["op"] == "adjust":
+        return {"bytes": 2 * N * V * (4 if case["dtype"] == "float32" else 2) + rules, "flops": 0}
+    H = case["H"]
+    fp8 = case.get("head", "fp8") == "fp8"
+    weight = V * H + -(-V // BLOCK) * -(-H // BLOCK) if fp8 else 2 * V * H
+    out = N * V * (4 if case["dtype"] == "float32" else 2) if case["op"] == "logits" else 29 * N + 20 * B
+    return {"bytes": weight + 2 * N * H + out + rules, "flops": 2 * N * V * H}
+
+
+# ---- the computed outputs in float64
+
+def _exact_weight(case, w):
+    """The weight that the case runs on, in float64: the bf16 one, or what its e4m3 blocks hold."""
+    if case.get("head") == "bf16":
+        return w.double()
+    q, scale = _quantised_weight(w)
+    step = torch.pow(torch.tensor(2.0, dtype=torch.float64, device="cuda"), scale.double() - 127.0)
+    step = step.repeat_interleave(BLOCK, 0)[:q.shape[0]]
+    out = q.double()
+    for k in range(step.shape[1]):
+        out[:, k * BLOCK:(k + 1) * BLOCK] *= step[:, k:k + 1]
+    return out
+
+
+def _exact_rows(hidden):
+    """bf16 rows rounded to e4m3 in blocks of 128, from the definition: the least 2^k with
+    |x| <= 448 * 2^k, nearest values, ties to even."""
+    x = hidden.double()
+    for lo in range(0, x.shape[1], BLOCK):
+        blk = x[:, lo:lo + BLOCK]
+        a = blk.abs().amax(1, keepdim=True)
+        m, e = torch.frexp(a / 448.0)                   # a / 448 = m 2^e, 0.5 <= m < 1
+        k = torch.where(m == 0.5, e - 1, e).clamp(min=-126).double()
+        y = blk * torch.exp2(-k)
+        _, ye = torch.frexp(y)
+        ulp = torch.exp2((ye.clamp(min=-5) - 4).double())   # 3 mantissa bits, subnormals from 2^-6
+        x[:, lo:lo + BLOCK] = torch.round(y / ulp) * ulp * torch.exp2(k)
+    return x
+
+
+def _exact_ruled(z, case, rules, parent, off, tok):
+    N, V = z.shape
+    counts = rules["counts"].long()
+    rep, pres, freq = (rules[k].double() for k in ("repetition", "presence", "frequency"))
+    toks = tok.tolist() if tok is not None else None
+    for b, (lo, hi) in enumerate(zip(off, off[1:])):
+        for n in range(lo, hi):
+            c = counts[b].clone()
+            j = n
+            while toks is not None and parent[j] >= 0:
+                c[toks[j]] += 1
+                j = parent[j]
+            row, k = z[n], c % PROMPT
+            row = torch.where(c > 0, torch.where(row > 0, row / rep[b], row * rep[b]), row)
+            row = row - torch.where(k > 0, pres[b] + freq[b] * k, 0.0) + rules["bias"][b].double()
+            if rules["allowed"] is not None:
+                bit = torch.arange(32, device="cuda")
+                on = ((rules["allowed"][n].long()[:, None] >> bit) & 1).view(-1)[:V] == 1
+                row = row.masked_fill(~on, -math.inf)
+            z[n] = row
+    return z
+
+
+def exact(case, seed):
+    if case["op"] == "counts":
+        return None
+    rng, gen = random.Random(seed), _gen(seed)
+    if case["op"] == "adjust":
+        s = _prepare_adjust(case, seed)
+        parent, off = _trees(case["B"], case["N"], rng) if case["tree"] else (None, list(range(case["N"] + 1)))
+        return _exact_ruled(s["logits"].double(), case, s["rules"], parent, off, s["tok"])
+    w, hidden, _ = _model(case, gen)
+    x = hidden.double() if case.get("head") == "bf16" else _exact_rows(hidden)
+    W = _exact_weight(case, w)
+    z = torch.cat([x @ W[lo:lo + 16384].T for lo in range(0, case["V"], 16384)], 1)
+    if case["op"] == "logits":
+        return z
+    del W
+    s = _prepare_verify(case, seed)
+    parent, off = _trees(case["B"], case["N"], rng)
+    if case["rules"]:
+        z = _exact_ruled(z, case, s["rules"], parent, off, s["tok"])
+    up = s["parent"].long()
+    drafted = z[up.clamp(min=0), s["tok"].long()].masked_fill(up < 0, 0.0)
+    return dict(row_max=z.amax(1), row_lse=torch.logsumexp(z, 1), row_argmax=None, drafted_logit=drafted,
+                accept=None, accepted_len=None, bonus_token=None, accepted_path=None, req_status=None)
