@@ -312,6 +312,133 @@ typedef struct asv_commit_args {
  * for bad sizes, null or misaligned pointers, ASV_EHIP if a launch fails. */
 int asv_commit(const asv_commit_args *args, void *stream);
 
+/* ---- Sampling rules and the 8-bit LM head. */
+
+/* An LM head in 8-bit floating point (OCP e4m3) with one power-of-two scale for each block of 128
+ * ids x 128 columns. asv_verify_ruled and asv_lm_head_logits round the hidden states alike, one
+ * scale for each row and 128 columns. The scale of a block is the least 2^e, e >= -126, with
+ * max |x| <= 448 * 2^e, kept as the byte e + 127 (OCP E8M0); each value x becomes the code nearest to
+ * x / 2^e, ties to even. A block with an infinity or a NaN gets the byte 255, and the logits that it
+ * enters are no numbers. Products are summed in fp32.
+ *
+ * The packed copy that the kernels read: with S = ceil(V / 256), codes in tiles of 256 ids x 64 columns,
+ *   packed[((k * S + s) * 256 + r) * 64 + 16 g + 8 h + c] = code[256 s + r][64 k + 32 h + 8 g + c]
+ * (g < 4, h < 2, c < 8), zero past V; then, from byte S * 256 * H on, the scale bytes of the 2 S
+ * blocks of 128 ids, 4 ceil(H / 512) bytes each. */
+#define ASV_W_FP8       2        /* asv_verify_args.w_lm_layout, in asv_verify_ruled only */
+
+/* Bytes of the packed copy. ASV_EINVAL for V <= 0, an H that asv_verify would reject, or codes of
+ * 4 GiB or more. */
+int asv_fp8_lm_head_bytes(int32_t V, int32_t H, uint64_t *bytes);
+
+/* Write the packed copy of the [V][H] bf16 weight w, quantised as above. Pointers 16-byte aligned,
+ * `packed` not overlapping the inputs. Enqueued on `stream`. ASV_EINVAL for bad sizes, null,
+ * misaligned or overlapping pointers or a packed_bytes too small; ASV_EHIP if the launch fails. */
+int asv_quantize_lm_head(const uint16_t *w, int32_t V, int32_t H, void *packed,
+                         uint64_t packed_bytes, void *stream);
+
+/* The same from a weight that is quantised already: e4m3 codes q [V][H] (16-byte aligned) and the
+ * scale bytes [ceil(V / 128)][ceil(H / 128)] of its blocks. */
+int asv_pack_fp8_lm_head(const uint8_t *q, const uint8_t *scale, int32_t V, int32_t H, void *packed,
+                         uint64_t packed_bytes, void *stream);
+
+/* Element types of logits in memory. */
+#define ASV_F32  0
+#define ASV_BF16 1
+#define ASV_F16  2
+
+/* Arguments of asv_lm_head_logits. */
+typedef struct asv_logits_args {
+  int32_t N, H, V;                /* host ints: N >= 0, H and V as in asv_verify */
+  int32_t out_type;               /* ASV_F32, ASV_BF16 or ASV_F16 */
+  const uint16_t *hidden;         /* [N][H] bf16, 16-byte aligned */
+  const void *w;                  /* the packed 8-bit LM head for this V and H, 16-byte aligned */
+  void *out;                      /* [N] rows of V logits, out_pitch elements apart; elements V ..
+                                     out_pitch - 1 of a row are left as they were */
+  int64_t out_pitch;              /* >= V */
+} asv_logits_args;
+
+/* z[n][v] = sum_h hidden[n][h] W[v][h] on the quantised values, N V logits in memory: for one token of
+ * each request (N = B) or whole trees. Workspace: asv_logits_workspace_bytes, 256-byte aligned, no
+ * initialisation needed; never falls as N grows. ASV_EINVAL for bad sizes or null or misaligned
+ * pointers (out: aligned to its elements), ASV_EWORKSPACE, or ASV_EHIP. */
+int asv_logits_workspace_bytes(int32_t N, int32_t H, int32_t V, uint64_t *bytes);
+int asv_lm_head_logits(const asv_logits_args *args, void *workspace, uint64_t workspace_bytes,
+                       void *stream);
+
+/* The history table of asv_token_counts: per request and id, how often the id was generated, plus
+ * ASV_COUNT_PROMPT if it occurs in the prompt. */
+#define ASV_COUNT_PROMPT (1 << 30)
+
+/* Sampling rules. With g = how often id v was generated in request b (counts) or drafted on the path
+ * from the root to node n (its own token included, the root's excluded), and seen = g > 0 or v in
+ * the prompt, the logit z[n][v] of row n becomes
+ *   z1 = seen ? (z > 0 ? z / repetition[b] : z * repetition[b]) : z
+ *   z2 = g > 0 ? z1 - (presence[b] + frequency[b] * g) : z1
+ *   z3 = z2 + bias[b][v]
+ *   z4 = bit v of allowed[n] set ? z3 : -inf
+ * in fp32, whatever z3 is. Every pointer may be NULL: no history, 1, 0, 0, no bias, all allowed. The
+ * values are applied as they are (a repetition of 0 divides by it). */
+typedef struct asv_logit_rules {
+  const int32_t *counts;          /* [B][V] history table */
+  const float *repetition;        /* [B] */
+  const float *presence;          /* [B] */
+  const float *frequency;         /* [B] */
+  const float *bias;              /* [V] for every request (bias_pitch 0), or [B] rows of V values,
+                                     bias_pitch floats apart */
+  int64_t bias_pitch;             /* 0 or >= V */
+  const uint32_t *allowed;        /* [N][ceil(V / 32)]: bit v % 32 of word v / 32 */
+} asv_logit_rules;
+
+/* asv_verify with sampling rules on the target's logits, and on an 8-bit LM head: with w_lm_layout =
+ * ASV_W_FP8, w_lm is the packed copy above (16-byte aligned). Every output is that of the ruled logits.
+ * With rules, a drafted token whose ruled logit is -inf is never accepted (at tau = 0 neither), and a row that
+ * they leave nothing has row_max = row_lse = -inf and row_argmax = -1, which is the bonus token of a
+ * walk that ends there. rules: NULL or all NULL for none. Workspace:
+ * asv_verify_ruled_workspace_bytes of the same layout; never falls as B, N or V grow. Results and
+ * errors otherwise as asv_verify's; ASV_EINVAL also for a bad bias_pitch, misaligned rules, or rules on
+ * more than 65535 rows. */
+int asv_verify_ruled_workspace_bytes(int32_t B, int32_t N, int32_t H, int32_t V,
+                                     int32_t w_lm_layout, uint64_t *bytes);
+int asv_verify_ruled(const asv_verify_args *args, const asv_logit_rules *rules, void *workspace,
+                     uint64_t workspace_bytes, void *stream);
+
+/* Arguments of asv_adjust_logits: the rules on logits in memory. */
+typedef struct asv_adjust_args {
+  int32_t B, N, V;                /* host ints: B >= 0, N >= B, V > 0, N and V < 2^30; without
+                                     req_offsets N == B */
+  int32_t type;                   /* ASV_F32, ASV_BF16 or ASV_F16, of in and out */
+  const void *in;                 /* [N] rows of V logits, in_pitch elements apart */
+  void *out;                      /* the same, out_pitch apart; may be `in` with the same pitch. Elements
+                                     V .. out_pitch - 1 of a row are left as they were */
+  int64_t in_pitch, out_pitch;    /* >= V */
+  const int32_t *req_offsets;     /* [B+1] as in asv_verify, or NULL: row n is request n */
+  const int32_t *parent;          /* [N] as in asv_verify, or NULL: no paths */
+  const int32_t *draft_tok;       /* [N]; NULL iff parent is */
+  asv_logit_rules rules;
+} asv_adjust_args;
+
+/* Apply the rules, in fp32, rounded once to the type. Rows that malformed offsets leave to no request
+ * are copied; a malformed link ends its row's path. ASV_EINVAL for bad sizes or null or misaligned
+ * pointers, ASV_EHIP if the launch fails. */
+int asv_adjust_logits(const asv_adjust_args *args, void *stream);
+
+/* Arguments of asv_token_counts. */
+typedef struct asv_counts_args {
+  int32_t B, T, V;                /* host ints: B >= 0, T >= 0, 0 < V < 2^30 */
+  int32_t add;                    /* 0: write the table; 1: add to it (asv_commit's tokens, say) */
+  const int32_t *tok;             /* [T] token ids */
+  const int32_t *tok_offsets;     /* [B+1]: request b's tokens are tok[tok_offsets[b]] .. up to
+                                     tok_offsets[b+1]; a request may have none */
+  const int32_t *prompt_len;      /* [B] how many of them are the prompt's, or NULL: none */
+  int32_t *counts;                /* [B][V] */
+  int32_t *req_status;            /* [B] ASV_RS_BAD_TOKEN (ids outside [0, V) are passed over),
+                                     ASV_RS_BAD_OFFSETS (offsets outside [0, T] or falling: the
+                                     request counts as empty) */
+} asv_counts_args;
+
+int asv_token_counts(const asv_counts_args *args, void *stream);
+
 /* ---- For callers that cannot allocate device memory (code under HIP graph capture, tight
  * serving loops, harnesses that forbid hipMalloc): asv_verify with its workspace taken from a
  * scratch array that the library holds in device memory, ASV_STATIC_SCRATCH_BYTES per GPU it

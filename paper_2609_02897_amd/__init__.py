@@ -12,10 +12,11 @@ import ctypes
 from typing import NamedTuple, Optional
 
 from ._abi import (  # noqa: F401
-    ASV_EHIP, ASV_EINVAL, ASV_ESCRATCH, ASV_EWORKSPACE, ASV_OK, DS_BAD_SHAPE, DS_OVERFLOW,
-    EXPORTS, LIB_PATH, POOL_MAX, RS_BAD_OFFSETS, RS_BAD_PARENT, RS_BAD_PATH, RS_BAD_ROOT,
-    RS_BAD_TAU, RS_BAD_TOKEN, RS_MASK_SMALL, STATIC_SCRATCH_BYTES, TOPK_MAX, W_PACKED,
-    W_ROW_MAJOR, AsvCommitArgs, AsvDraftArgs, AsvDraftTree, AsvParams, AsvReqState, AsvTuning,
+    ASV_EHIP, ASV_EINVAL, ASV_ESCRATCH, ASV_EWORKSPACE, ASV_OK, BF16, COUNT_PROMPT, DS_BAD_SHAPE,
+    DS_OVERFLOW, EXPORTS, F16, F32, LIB_PATH, POOL_MAX, RS_BAD_OFFSETS, RS_BAD_PARENT,
+    RS_BAD_PATH, RS_BAD_ROOT, RS_BAD_TAU, RS_BAD_TOKEN, RS_MASK_SMALL, STATIC_SCRATCH_BYTES,
+    TOPK_MAX, W_FP8, W_PACKED, W_ROW_MAJOR, AsvAdjustArgs, AsvCommitArgs, AsvCountsArgs,
+    AsvDraftArgs, AsvDraftTree, AsvLogitRules, AsvLogitsArgs, AsvParams, AsvReqState, AsvTuning,
     AsvVerifyArgs, LibraryMissing, load)
 
 STATE_BYTES = ctypes.sizeof(AsvReqState)
@@ -68,16 +69,20 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def workspace_bytes(B: int, N: int, H: int, V: int) -> int:
+def workspace_bytes(B: int, N: int, H: int, V: int, w_lm=None) -> int:
+    """Workspace of ``verify``; with ``w_lm``, for this weight (the 8-bit one needs more)."""
     out = ctypes.c_uint64(0)
-    _check(load().asv_workspace_bytes(B, N, H, V, ctypes.byref(out)))
+    if isinstance(w_lm, PackedLmHead) and w_lm.kind == "fp8":
+        _check(load().asv_verify_ruled_workspace_bytes(B, N, H, V, W_FP8, ctypes.byref(out)))
+    else:
+        _check(load().asv_workspace_bytes(B, N, H, V, ctypes.byref(out)))
     return int(out.value)
 
 
-def alloc_workspace(B: int, N: int, H: int, V: int, device):
-    """A workspace tensor for asv_verify (torch allocations are 256-byte aligned)."""
+def alloc_workspace(B: int, N: int, H: int, V: int, device, w_lm=None):
+    """A workspace tensor for ``verify`` (torch allocations are 256-byte aligned)."""
     import torch
-    n = max(workspace_bytes(B, N, H, V), 256)
+    n = max(workspace_bytes(B, N, H, V, w_lm), 256)
     ws = torch.empty(n, dtype=torch.uint8, device=device)
     assert ws.data_ptr() % 256 == 0
     return ws
@@ -173,9 +178,11 @@ def _same_device(device, **tensors):
 
 class PackedLmHead(NamedTuple):
     """An LM-head weight in a packed tile layout: ``kind`` "target" (``asv_pack_lm_head``,
-    [256 rows][64 columns] tiles, for ``verify``) or "draft" (``asv_pack_draft_head``, [64][64]
-    tiles, for ``draft_step``). Tiles are stored 64-column block major, zero rows past V."""
-    data: "torch.Tensor"             # bf16, flat, packed_*_bytes(V, H) / 2 values
+    [256 rows][64 columns] tiles, for ``verify``), "draft" (``asv_pack_draft_head``, [64][64]
+    tiles, for ``draft_step``) or "fp8" (e4m3 codes in [256][128] tiles and the scales of their
+    128 x 128 blocks, for ``verify`` and ``lm_head_logits``). Tiles are stored column block major,
+    zero rows past V."""
+    data: "torch.Tensor"             # flat: bf16, packed_*_bytes(V, H) / 2 values; "fp8": uint8
     V: int
     H: int
     kind: str
@@ -184,7 +191,8 @@ class PackedLmHead(NamedTuple):
 def packed_lm_head_bytes(V: int, H: int, kind: str = "target") -> int:
     out = ctypes.c_uint64()
     lib = load()
-    f = lib.asv_packed_lm_head_bytes if kind == "target" else lib.asv_packed_draft_head_bytes
+    f = {"target": lib.asv_packed_lm_head_bytes, "draft": lib.asv_packed_draft_head_bytes,
+         "fp8": lib.asv_fp8_lm_head_bytes}[kind]
     _check(f(V, H, ctypes.byref(out)))
     return out.value
 
@@ -214,9 +222,47 @@ def pack_draft_head(w_draft) -> PackedLmHead:
     return _pack(w_draft, "draft")
 
 
-def _weight(w, kind: str, name: str, H: int):
-    """(pointer, V, layout) of a row-major [V, H] weight or its packed copy of this kind."""
+def quantize_lm_head(w_lm) -> PackedLmHead:
+    """A bf16 [V, H] LM-head weight in 8-bit floating point (``asv_quantize_lm_head``): e4m3 codes, one
+    power-of-two scale for each 128 x 128 block, packed for ``verify`` and ``lm_head_logits``."""
     import torch
+    V, H = w_lm.shape
+    _need(w_lm, "weight", torch.bfloat16, (V, H))
+    data = torch.empty(packed_lm_head_bytes(V, H, "fp8"), dtype=torch.uint8, device=w_lm.device)
+    with torch.cuda.device(w_lm.device):
+        _check(load().asv_quantize_lm_head(w_lm.data_ptr(), V, H, data.data_ptr(), data.numel(),
+                                           _stream_handle(w_lm.device)))
+    return PackedLmHead(data, V, H, "fp8")
+
+
+def pack_lm_head_fp8(q, scale) -> PackedLmHead:
+    """The packed copy of an LM head that a checkpoint holds in 8 bits (``asv_pack_fp8_lm_head``): q
+    float8_e4m3fn [V, H]; scale [ceil(V / 128), ceil(H / 128)], float8_e8m0fnu or its bytes (uint8): block
+    (i, j) of 128 x 128 stands for q * 2^(scale[i, j] - 127)."""
+    import torch
+    V, H = q.shape
+    _need(q, "q", torch.float8_e4m3fn, (V, H))
+    if isinstance(scale, torch.Tensor) and scale.dtype == torch.float8_e8m0fnu:
+        scale = scale.view(torch.uint8)
+    _need(scale, "scale", torch.uint8, (-(-V // 128), -(-H // 128)))
+    if scale.device != q.device:
+        raise ValueError(f"scale: on {scale.device}, the codes are on {q.device}")
+    data = torch.empty(packed_lm_head_bytes(V, H, "fp8"), dtype=torch.uint8, device=q.device)
+    with torch.cuda.device(q.device):
+        _check(load().asv_pack_fp8_lm_head(q.data_ptr(), scale.data_ptr(), V, H, data.data_ptr(),
+                                           data.numel(), _stream_handle(q.device)))
+    return PackedLmHead(data, V, H, "fp8")
+
+
+def _weight(w, kind: str, name: str, H: int):
+    """(pointer, V, layout) of a row-major [V, H] weight or its packed copy of this kind; where the
+    target's is asked for, also of its 8-bit copy."""
+    import torch
+    if isinstance(w, PackedLmHead) and w.kind == "fp8" and kind == "target":
+        if w.H != H:
+            raise ValueError(f"{name}: packed for H = {w.H}, the hidden states have H = {H}")
+        _need(w.data, f"{name}.data", torch.uint8, (packed_lm_head_bytes(w.V, H, "fp8"),))
+        return w.data.data_ptr(), w.V, W_FP8
     if isinstance(w, PackedLmHead):
         if w.kind != kind:
             raise ValueError(f"{name}: packed for the {w.kind} LM head, not the {kind}")
@@ -233,12 +279,14 @@ def _weight(w, kind: str, name: str, H: int):
 def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None, state=None,
            params: Optional[AsvParams] = None, out: Optional[VerifyOut] = None,
            workspace=None, k1_events=None, k1_tile: int = 0,
-           noalloc: bool = False) -> VerifyOut:
+           noalloc: bool = False, rules: Optional["LogitRules"] = None) -> VerifyOut:
     """One verification step through ``asv_verify`` on torch's current stream.
 
-    hidden bf16 [N, H]; w_lm bf16 [V, H] or its ``PackedLmHead``; draft_tok, parent int32 [N];
-    req_offsets int32 [B+1]; tau float32 [B]; draft_logits float32 [N, V] or None; state u8
-    [B, 112] (in/out) or None. ``out`` and ``workspace`` may be passed to reuse buffers
+    hidden bf16 [N, H]; w_lm bf16 [V, H], its ``PackedLmHead`` or an 8-bit one; draft_tok, parent int32
+    [N]; req_offsets int32 [B+1]; tau float32 [B]; draft_logits float32 [N, V] or None; state u8
+    [B, 112] (in/out) or None; rules ``LogitRules`` or None. Rules and the 8-bit weight go through
+    ``asv_verify_ruled``, where every output is that of the ruled logits; they take no events,
+    forced tile or ``noalloc``. ``out`` and ``workspace`` may be passed to reuse buffers
     (checked against these sizes). Measurement and tuning go through ``asv_verify_tuned``:
     ``k1_events`` is an optional pair of raw hipEvent_t handles set to the start and end of
     the LM-head kernel's launches, and ``k1_tile`` forces the LM-head tile (64, 128, 192 or 256 tree rows); 0 lets the
@@ -253,6 +301,9 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
     B = req_offsets.shape[0] - 1
     _need(hidden, "hidden", torch.bfloat16, (N, H))
     w_ptr, V, layout = _weight(w_lm, "target", "w_lm", H)
+    ruled = rules is not None or layout == W_FP8
+    if ruled and (noalloc or k1_events is not None or k1_tile):
+        raise ValueError("rules and the 8-bit weight take no noalloc, events or forced tile")
     _need(draft_tok, "draft_tok", torch.int32, (N,))
     _need(parent, "parent", torch.int32, (N,))
     _need(req_offsets, "req_offsets", torch.int32, (B + 1,))
@@ -272,9 +323,9 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
     if noalloc:
         pass
     elif workspace is None:
-        workspace = alloc_workspace(B, N, H, V, dev)
+        workspace = alloc_workspace(B, N, H, V, dev, w_lm)
     else:
-        _need_workspace(workspace, workspace_bytes(B, N, H, V), dev)
+        _need_workspace(workspace, workspace_bytes(B, N, H, V, w_lm), dev)
     a = AsvVerifyArgs()
     a.B, a.N, a.H, a.V = B, N, H, V
     a.hidden, a.w_lm, a.w_lm_layout = hidden.data_ptr(), w_ptr, layout
@@ -291,7 +342,12 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
     a.req_status = out.req_status.data_ptr()
     a.params = params or make_params()
     lib = load()
-    if noalloc:
+    if ruled:
+        r = _rules(rules, B, N, V, dev)
+        with torch.cuda.device(dev):
+            _check(lib.asv_verify_ruled(ctypes.byref(a), ctypes.byref(r), workspace.data_ptr(),
+                                        workspace.numel(), _stream_handle(dev)))
+    elif noalloc:
         _check(lib.asv_verify_noalloc(ctypes.byref(a), _stream_handle(dev)))
     elif k1_events is None and not k1_tile:
         _check(lib.asv_verify(ctypes.byref(a), workspace.data_ptr(), workspace.numel(),
@@ -302,6 +358,182 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
                                     workspace.numel(), _stream_handle(dev)))
     return out
 
+
+# ----------------------------------------------------------------------------- sampling rules
+
+class LogitRules(NamedTuple):
+    """Sampling rules of B requests with N rows on V ids (``asv_logit_rules``); None leaves one out.
+    With g = how often an id was generated (``counts``) or drafted on the row's path and seen = g > 0
+    or in the prompt: the logit of a seen id is divided by ``repetition`` if positive, else
+    multiplied by it; an id with g > 0 loses presence + frequency * g; then the bias is added; ids
+    whose bit is not set get -inf."""
+    counts: Optional["torch.Tensor"] = None       # i32 [B, V], from token_counts
+    repetition: Optional["torch.Tensor"] = None   # f32 [B]
+    presence: Optional["torch.Tensor"] = None     # f32 [B]
+    frequency: Optional["torch.Tensor"] = None    # f32 [B]
+    bias: Optional["torch.Tensor"] = None         # f32 [V] or [B, V], rows any stride >= V apart
+    allowed: Optional["torch.Tensor"] = None      # i32 [N, ceil(V / 32)], bit v % 32 of word v / 32
+
+
+def _rules(rules: Optional[LogitRules], B: int, N: int, V: int, device) -> AsvLogitRules:
+    import torch
+    r = AsvLogitRules()
+    if rules is None:
+        return r
+    f32, i32 = torch.float32, torch.int32
+    for name, dtype, shape in (("counts", i32, (B, V)), ("repetition", f32, (B,)),
+                               ("presence", f32, (B,)), ("frequency", f32, (B,)),
+                               ("allowed", i32, (N, -(-V // 32)))):
+        t = getattr(rules, name)
+        if t is not None:
+            _need(t, f"rules.{name}", dtype, shape)
+            setattr(r, name, t.data_ptr())
+    t = rules.bias
+    if t is not None:
+        if isinstance(t, torch.Tensor) and t.dim() == 2:
+            r.bias_pitch = _need_rows(t, "rules.bias", f32, (B, V))
+        else:
+            _need(t, "rules.bias", f32, (V,))
+        r.bias = t.data_ptr()
+    for name, t in zip(rules._fields, rules):
+        if t is not None and t.device != device:
+            raise ValueError(f"rules.{name}: on {t.device}, the rows are on {device}")
+    return r
+
+
+def _need_rows(t, name, dtype, shape) -> int:
+    """A GPU matrix whose rows are contiguous, any stride of at least a row apart: the stride."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be on a GPU (no CPU path exists)")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row must be contiguous")
+    pitch = t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    if pitch < cols:
+        raise ValueError(f"{name}: rows overlap")
+    return pitch
+
+
+def _logits_type(dtype) -> int:
+    import torch
+    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if dtype not in types:
+        raise TypeError(f"logits: float32, bfloat16 or float16, not {dtype}")
+    return types[dtype]
+
+
+def logits_workspace_bytes(N: int, H: int, V: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(load().asv_logits_workspace_bytes(N, H, V, ctypes.byref(out)))
+    return int(out.value)
+
+
+def lm_head_logits(hidden, w_lm: PackedLmHead, dtype=None, out=None, workspace=None):
+    """The logits [N, V] of bf16 hidden states [N, H] on an 8-bit LM head (``asv_lm_head_logits``, torch's
+    current stream), as ``dtype`` (float32 unless ``out`` says otherwise). ``out``: a matrix to write
+    to, rows any stride >= V apart."""
+    import torch
+    N, H = hidden.shape
+    _need(hidden, "hidden", torch.bfloat16, (N, H))
+    if not isinstance(w_lm, PackedLmHead) or w_lm.kind != "fp8":
+        raise TypeError("w_lm: an 8-bit PackedLmHead (quantize_lm_head, pack_lm_head_fp8)")
+    w_ptr, V, _ = _weight(w_lm, "target", "w_lm", H)
+    dev = hidden.device
+    _same_device(dev, w_lm=w_lm.data, out=out)
+    if out is None:
+        out = torch.empty((N, V), dtype=dtype or torch.float32, device=dev)
+    elif dtype is not None and out.dtype != dtype:
+        raise TypeError(f"out: expected {dtype}, got {out.dtype}")
+    a = AsvLogitsArgs()
+    a.N, a.H, a.V, a.out_type = N, H, V, _logits_type(out.dtype)
+    a.out_pitch = _need_rows(out, "out", out.dtype, (N, V))
+    a.hidden, a.w, a.out = hidden.data_ptr(), w_ptr, out.data_ptr()
+    need = logits_workspace_bytes(N, H, V)
+    if workspace is None:
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    else:
+        _need_workspace(workspace, need, dev)
+    with torch.cuda.device(dev):
+        _check(load().asv_lm_head_logits(ctypes.byref(a), workspace.data_ptr(), workspace.numel(),
+                                         _stream_handle(dev)))
+    return out
+
+
+def adjust_logits(logits, rules: LogitRules, req_offsets=None, parent=None, draft_tok=None,
+                  out=None):
+    """Sampling rules on logits in memory (``asv_adjust_logits``, torch's current stream): float32,
+    bfloat16 or float16 [N, V], rows any stride >= V apart. Row n belongs to the request of
+    req_offsets int32 [B+1], or to request n without it; with a tree's parent and draft_tok int32 [N],
+    a row also counts the tokens drafted on its path. ``out``: a matrix of the same type and shape, may be ``logits``
+    itself; a new one by default."""
+    import torch
+    N, V = logits.shape
+    B = N if req_offsets is None else req_offsets.shape[0] - 1
+    if (parent is None) != (draft_tok is None):
+        raise ValueError("parent and draft_tok: both or neither")
+    if parent is not None and req_offsets is None:
+        raise ValueError("a tree needs req_offsets")
+    a = AsvAdjustArgs()
+    a.B, a.N, a.V, a.type = B, N, V, _logits_type(logits.dtype)
+    a.in_pitch = _need_rows(logits, "logits", logits.dtype, (N, V))
+    dev = logits.device
+    if out is None:
+        out = torch.empty((N, V), dtype=logits.dtype, device=dev)
+    a.out_pitch = _need_rows(out, "out", logits.dtype, (N, V))
+    for name, t, n in (("req_offsets", req_offsets, B + 1), ("parent", parent, N),
+                       ("draft_tok", draft_tok, N)):
+        if t is not None:
+            _need(t, name, torch.int32, (n,))
+            setattr(a, name, t.data_ptr())
+    for name, t in (("out", out), ("req_offsets", req_offsets), ("parent", parent),
+                    ("draft_tok", draft_tok)):
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, the logits are on {dev}")
+    a.in_, a.out = logits.data_ptr(), out.data_ptr()
+    a.rules = _rules(rules, B, N, V, dev)
+    with torch.cuda.device(dev):
+        _check(load().asv_adjust_logits(ctypes.byref(a), _stream_handle(dev)))
+    return out
+
+
+def token_counts(tokens, offsets, V: int, prompt_len=None, counts=None):
+    """``asv_token_counts``: (counts [B, V], req_status [B]), the history table of the rules. tokens int32 [T];
+    offsets int32 [B+1]: request b's tokens; prompt_len int32 [B]: how many of them are the
+    prompt's (default none). With ``counts``, the tokens are added to that table in place, e.g. the tokens and
+    offsets that ``commit`` returned."""
+    import torch
+    T, B = tokens.shape[0], offsets.shape[0] - 1
+    _need(tokens, "tokens", torch.int32, (T,))
+    _need(offsets, "offsets", torch.int32, (B + 1,))
+    dev = tokens.device
+    a = AsvCountsArgs()
+    a.B, a.T, a.V, a.add = B, T, V, int(counts is not None)
+    if prompt_len is not None:
+        _need(prompt_len, "prompt_len", torch.int32, (B,))
+        a.prompt_len = prompt_len.data_ptr()
+    if counts is None:
+        counts = torch.empty((B, V), dtype=torch.int32, device=dev)
+    else:
+        _need(counts, "counts", torch.int32, (B, V))
+    for name, t in (("offsets", offsets), ("prompt_len", prompt_len), ("counts", counts)):
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, the tokens are on {dev}")
+    status = torch.empty(B, dtype=torch.int32, device=dev)
+    a.tok, a.tok_offsets = tokens.data_ptr(), offsets.data_ptr()
+    a.counts, a.req_status = counts.data_ptr(), status.data_ptr()
+    with torch.cuda.device(dev):
+        _check(load().asv_token_counts(ctypes.byref(a), _stream_handle(dev)))
+    return counts, status
+
+
+# ----------------------------------------------------------------------------- LM-head launches
 
 def k1_plan(N: int, V: int, cus: int, tile_rows: int = 0) -> list:
     """The plan of ``verify``'s LM-head launches over whole 256-id slabs, for N tree rows and V

@@ -10,7 +10,9 @@ LIB_PATH = os.path.join(_HERE, "libasv.so")
 
 ASV_OK, ASV_EINVAL, ASV_EWORKSPACE, ASV_EHIP, ASV_ESCRATCH = 0, -1, -2, -3, -4
 STATIC_SCRATCH_BYTES = 32 << 20   # ASV_STATIC_SCRATCH_BYTES
-W_ROW_MAJOR, W_PACKED = 0, 1     # asv_verify_args.w_lm_layout
+W_ROW_MAJOR, W_PACKED, W_FP8 = 0, 1, 2     # asv_verify_args.w_lm_layout
+F32, BF16, F16 = 0, 1, 2                   # element types of logits
+COUNT_PROMPT = 1 << 30                     # history table: the id occurs in the prompt
 RS_BAD_ROOT, RS_BAD_PARENT, RS_BAD_TOKEN, RS_BAD_OFFSETS, RS_BAD_TAU = 1, 2, 4, 16, 32
 RS_MASK_SMALL, RS_BAD_PATH = 64, 128
 DS_BAD_SHAPE, DS_OVERFLOW = 1, 2
@@ -23,7 +25,10 @@ EXPORTS = ("asv_version", "asv_status_string", "asv_last_error", "asv_workspace_
            "asv_draft_step", "asv_draft_prune", "asv_tree_meta", "asv_commit",
            "asv_packed_lm_head_bytes", "asv_pack_lm_head", "asv_packed_draft_head_bytes",
            "asv_pack_draft_head", "asv_verify_tuned", "asv_draft_step_tuned",
-           "asv_verify_noalloc", "asv_k1_plan", "asv_k1_cut", "asv_draft_cut")
+           "asv_verify_noalloc", "asv_k1_plan", "asv_k1_cut", "asv_draft_cut",
+           "asv_fp8_lm_head_bytes", "asv_quantize_lm_head", "asv_pack_fp8_lm_head",
+           "asv_logits_workspace_bytes", "asv_lm_head_logits", "asv_verify_ruled_workspace_bytes",
+           "asv_verify_ruled", "asv_adjust_logits", "asv_token_counts")
 
 
 class AsvReqState(ctypes.Structure):
@@ -97,6 +102,30 @@ class AsvCommitArgs(ctypes.Structure):
                 ("bonus_token", _P), ("commit_off", _P), ("commit_tok", _P),
                 ("commit_row", _P), ("row_src", _P), ("row_dst", _P),
                 ("row_bytes", ctypes.c_int64), ("req_status", _P)]
+
+
+class AsvLogitsArgs(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int32), ("H", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("out_type", ctypes.c_int32), ("hidden", _P), ("w", _P), ("out", _P),
+                ("out_pitch", ctypes.c_int64)]
+
+
+class AsvLogitRules(ctypes.Structure):
+    _fields_ = [("counts", _P), ("repetition", _P), ("presence", _P), ("frequency", _P),
+                ("bias", _P), ("bias_pitch", ctypes.c_int64), ("allowed", _P)]
+
+
+class AsvAdjustArgs(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("in_", _P), ("out", _P), ("in_pitch", ctypes.c_int64),
+                ("out_pitch", ctypes.c_int64), ("req_offsets", _P), ("parent", _P),
+                ("draft_tok", _P), ("rules", AsvLogitRules)]
+
+
+class AsvCountsArgs(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32),
+                ("add", ctypes.c_int32), ("tok", _P), ("tok_offsets", _P), ("prompt_len", _P),
+                ("counts", _P), ("req_status", _P)]
 
 
 assert ctypes.sizeof(AsvReqState) == 112
@@ -174,5 +203,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     for f in (lib.asv_pack_lm_head, lib.asv_pack_draft_head):
         f.restype = ctypes.c_int
         f.argtypes = [_P, ctypes.c_int32, ctypes.c_int32, _P, ctypes.c_uint64, _P]
+    i32, u64, size = ctypes.c_int32, ctypes.c_uint64, ctypes.POINTER(ctypes.c_uint64)
+    for name, args in (
+            ("asv_fp8_lm_head_bytes", [i32, i32, size]),
+            ("asv_quantize_lm_head", [_P, i32, i32, _P, u64, _P]),
+            ("asv_pack_fp8_lm_head", [_P, _P, i32, i32, _P, u64, _P]),
+            ("asv_logits_workspace_bytes", [i32, i32, i32, size]),
+            ("asv_lm_head_logits", [ctypes.POINTER(AsvLogitsArgs), _P, u64, _P]),
+            ("asv_verify_ruled_workspace_bytes", [i32] * 5 + [size]),
+            ("asv_verify_ruled", [ctypes.POINTER(AsvVerifyArgs), ctypes.POINTER(AsvLogitRules), _P,
+                                  u64, _P]),
+            ("asv_adjust_logits", [ctypes.POINTER(AsvAdjustArgs), _P]),
+            ("asv_token_counts", [ctypes.POINTER(AsvCountsArgs), _P])):
+        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib

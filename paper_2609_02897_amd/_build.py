@@ -7,17 +7,19 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
-SOURCES = [os.path.join(_HERE, "csrc", "asv_api.hip")]
+SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("asv_api.hip", "asv_logits.hip",
+                                                                "asv_rules.hip")]
 HEADERS = [os.path.join(ROOT, "include", "asv.h")] + [
-    os.path.join(_HERE, "csrc", f) for f in ("k_common.h", "k_lmhead.h", "k_reduce.h",
-                                               "k_accept.h", "k_draft.h", "k_tree.h")]
+    os.path.join(_HERE, "csrc", f) for f in ("asv_host.h", "asv_k1_host.h", "k_common.h",
+                                               "k_lmhead.h", "k_reduce.h", "k_accept.h",
+                                               "k_draft.h", "k_tree.h", "k_rules.h", "k_fp8.h")]
 OUT = os.path.join(_HERE, "libasv.so")
 # measurement-only library (achievable-peak microbenchmarks), separate from libasv
 MICROBENCH_SOURCES = [os.path.join(_HERE, "csrc", "microbench.hip")]
 MICROBENCH_OUT = os.path.join(_HERE, "libasv_microbench.so")
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # code objects every ROCm 7.x runtime loads (torch may bring an older runtime than hipcc)
     "-mcode-object-version=5",
     # keep the compiler from forming packed fp32 (v_pk_*_f32) instructions
@@ -33,13 +35,29 @@ def hipcc() -> str:
 def build_library(out: str = OUT, verbose: bool = False, sources=None) -> str:
     """Compile the HIP sources (libasv's by default) into ``out`` (written atomically)."""
     tmp = out + ".tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-o", tmp,
-           *(sources or SOURCES)]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = "\n".join(l for l in (res.stdout + res.stderr).splitlines()
-                     if "packed-fp32-ops" not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{' '.join(cmd)}\n{msgs}")
+    sources = sources or SOURCES
+    objects = [f"{tmp}{i}.o" for i in range(len(sources))]
+    flags = [*HIPCC_FLAGS, "-I", os.path.join(ROOT, "include")]
+    msgs = ""
+
+    def run(cmds):                  # side by side
+        nonlocal msgs
+        procs = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                 for c in cmds]
+        outs = [p.communicate()[0] for p in procs]
+        for c, p, o in zip(cmds, procs, outs):
+            o = "\n".join(l for l in o.splitlines() if "packed-fp32-ops" not in l)
+            if p.returncode != 0:
+                raise RuntimeError(f"hipcc failed ({p.returncode}):\n{' '.join(c)}\n{o}")
+            msgs += o
+
+    try:
+        run([[hipcc(), *flags, "-c", src, "-o", obj] for src, obj in zip(sources, objects)])
+        run([[hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *objects]])
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     if verbose and msgs.strip():
         print(msgs)
     os.replace(tmp, out)

@@ -277,6 +277,22 @@ __device__ __forceinline__ void finish_request(const AcceptArgs& a, int b, int n
     reinterpret_cast<uint32_t*>(a.state + b)[lane] = reinterpret_cast<const uint32_t*>(&q)[lane];
 }
 
+// Eq. (1) for a node with drafted logit g under a row of maximum mx. Under sampling rules (RULED) a
+// token that they rule out (a logit of -inf) is never accepted, not even at kappa = 0.
+template <bool RULED>
+__device__ __forceinline__ bool node_ok(bool top1, float kappa, float g, float mx, float ln_kappa) {
+  const bool ok = top1 || kappa == 0.f || g - mx >= ln_kappa;
+  if constexpr (RULED) return ok && g != kNegInf;
+  else return ok;
+}
+
+// The argmax of a row: under sampling rules -1 where they leave the row nothing.
+template <bool RULED>
+__device__ __forceinline__ int row_arg_of(int a) {
+  if constexpr (RULED) return a == kNoIndex ? -1 : a;
+  else return a;
+}
+
 // Ordered key of a child: larger drafted logit first, then the lower node index. -0 is folded
 // into +0 so that equal logits compare equal.
 __device__ __forceinline__ uint64_t child_key(float g, int i) {
@@ -306,6 +322,7 @@ __device__ __forceinline__ void stage_inputs(const AcceptArgs& a, int b, int lo,
 // Request b with rows [lo, hi), 0 <= lo < hi <= N and n = hi - lo <= kWaveStage, with its
 // inputs in `in` (stage_inputs). Loads the row max / argmax of the request's rows, then walks
 // in LDS. Every lane of the wave calls this with the same arguments.
+template <bool RULED>
 __device__ __forceinline__ void accept_staged(const AcceptArgs& a, int b, int lo, int hi, int lane,
                                               WalkSmem& sm, const WalkInputs& in) {
   const int n = hi - lo;
@@ -349,7 +366,7 @@ __device__ __forceinline__ void accept_staged(const AcceptArgs& a, int b, int lo
   for (int i = 1 + lane; i < n; i += kWave) {
     const int p = sm.par[i] - lo;
     const float gi = sm.g[i];
-    const bool ok = (sm.tok[i] == sm.arg[p]) || kappa == 0.f || (gi - sm.mx[p] >= ln_kappa);
+    const bool ok = node_ok<RULED>(sm.tok[i] == sm.arg[p], kappa, gi, sm.mx[p], ln_kappa);
     sm.ok[i] = ok;
     a.accept[lo + i] = ok;
     atomicMax(reinterpret_cast<unsigned long long*>(&sm.best[p]),
@@ -394,6 +411,7 @@ __device__ __forceinline__ void best_child_reduce(float& g, int& c) {
 
 // Request b with more than kWaveStage nodes: the same steps, reading global memory, with one
 // wave-wide best-child reduction per walk step. Only the state words are staged (sm.st).
+template <bool RULED>
 __device__ __forceinline__ void accept_global(const AcceptArgs& a, int b, int lo, int hi, int lane,
                               WalkSmem& sm) {
   const int n = hi - lo;
@@ -429,7 +447,7 @@ __device__ __forceinline__ void accept_global(const AcceptArgs& a, int b, int lo
     uint8_t ok = 1;
     if (c != lo) {
       const int p = a.parent[c];
-      ok = (a.tok[c] == Ar(p)) || kappa == 0.f || (a.g[c] - Mr(p) >= ln_kappa);
+      ok = node_ok<RULED>(a.tok[c] == Ar(p), kappa, a.g[c], Mr(p), ln_kappa);
     }
     a.accept[c] = ok;
   }
@@ -451,7 +469,7 @@ __device__ __forceinline__ void accept_global(const AcceptArgs& a, int b, int lo
     if (bc == kNoIndex) break;
     const int arg = Ar(cur);
     const int d = a.tok[bc];
-    const bool ok = (d == arg) || kappa == 0.f || (bg - Mr(cur) >= ln_kappa);
+    const bool ok = node_ok<RULED>(d == arg, kappa, bg, Mr(cur), ln_kappa);
     if (!ok) break;
     if (d != arg) {
       if (a.prm.max_promotions >= 0 && promos >= a.prm.max_promotions) break;
@@ -484,6 +502,7 @@ constexpr int kFinishWaves = 4;    // rows per workgroup, one wave per row
 // stores, and every wave waits for its stores to complete before the workgroup barrier that
 // precedes the counter update; the completing wave reads them with device-coherent loads
 // issued after the counter's returned value is known.
+template <bool RULED>
 __global__ __launch_bounds__(kFinishWaves * kWave)
 void k_merge_accept(int S, const float* __restrict__ rec_m, const float* __restrict__ rec_s,
                     const int32_t* __restrict__ rec_a, float* row_max, float* __restrict__ row_lse,
@@ -505,7 +524,7 @@ void k_merge_accept(int S, const float* __restrict__ rec_m, const float* __restr
     if (lane == 0) {
       st_device(row_max + n, r.m);
       row_lse[n] = r.m + __builtin_amdgcn_logf(r.s) * 0.69314718055994531f;
-      st_device(row_argmax + n, r.a);
+      st_device(row_argmax + n, row_arg_of<RULED>(r.a));
     }
   }
 
@@ -552,9 +571,9 @@ void k_merge_accept(int S, const float* __restrict__ rec_m, const float* __restr
   }
   if (!__builtin_amdgcn_readfirstlane(done)) return;
   if (staged)
-    accept_staged(a, b, lo, hi, lane, s_walk[w], in);
+    accept_staged<RULED>(a, b, lo, hi, lane, s_walk[w], in);
   else
-    accept_global(a, b, lo, hi, lane, s_walk[w]);
+    accept_global<RULED>(a, b, lo, hi, lane, s_walk[w]);
 }
 
 // ---- unfused finishing step, for batches beyond kFusedMaxB requests
@@ -563,6 +582,7 @@ constexpr int kMergeRowsPerBlock = 4;  // one wave per row
 
 // Grid ceil(N / 4): merges one row per wave, and checks a slice of the offsets, raising
 // *bad_flag (cleared by the LM-head kernel) when any pair is malformed.
+template <bool RULED>
 __global__ __launch_bounds__(kMergeRowsPerBlock * kWave)
 void k_slab_merge(int N, int S, const float* __restrict__ rec_m, const float* __restrict__ rec_s,
                   const int32_t* __restrict__ rec_a, float* __restrict__ row_max,
@@ -580,11 +600,12 @@ void k_slab_merge(int N, int S, const float* __restrict__ rec_m, const float* __
   if (lane == 0) {
     row_max[n] = r.m;
     row_lse[n] = r.m + __builtin_amdgcn_logf(r.s) * 0.69314718055994531f;
-    row_argmax[n] = r.a;
+    row_argmax[n] = row_arg_of<RULED>(r.a);
   }
 }
 
 // Grid B, one wave per request.
+template <bool RULED>
 __global__ __launch_bounds__(kWave)
 void k_tree_accept(const int32_t* __restrict__ bad_flag, AcceptArgs a) {
   __shared__ WalkSmem s_walk;
@@ -597,12 +618,12 @@ void k_tree_accept(const int32_t* __restrict__ bad_flag, AcceptArgs a) {
   if (hi - lo <= kWaveStage) {
     WalkInputs in;
     stage_inputs(a, b, lo, lane, in);
-    accept_staged(a, b, lo, hi, lane, s_walk, in);
+    accept_staged<RULED>(a, b, lo, hi, lane, s_walk, in);
   } else
-    accept_global(a, b, lo, hi, lane, s_walk);
+    accept_global<RULED>(a, b, lo, hi, lane, s_walk);
 }
 
-__global__ void k_state_init(asv_req_state* state, int B, asv_params prm) {
+static __global__ void k_state_init(asv_req_state* state, int B, asv_params prm) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= B) return;
   asv_req_state* s = state + b;
@@ -620,7 +641,7 @@ __global__ void k_state_init(asv_req_state* state, int B, asv_params prm) {
 }
 
 // Grid-stride over requests: optional fresh draft confidence, then the tree shape.
-__global__ void k_tree_policy(const float* __restrict__ conf, asv_req_state* state, int B,
+static __global__ void k_tree_policy(const float* __restrict__ conf, asv_req_state* state, int B,
                               asv_params prm) {
   for (int b = blockIdx.x * blockDim.x + threadIdx.x; b < B; b += gridDim.x * blockDim.x) {
     asv_req_state q = state[b];

@@ -29,6 +29,7 @@
 
 #include "k_common.h"
 #include "k_reduce.h"
+#include "k_rules.h"
 
 namespace asv {
 
@@ -648,6 +649,8 @@ struct LmheadArgs {
   int n_cnt;
   int w_packed;                  // 0: W row-major; else packed, V rounded up to this many rows
   ConfArgs conf;                 // the draft logits' records that 64-row tiles also write
+  const uint8_t* w_scale;        // scale bytes of an 8-bit W (see k_fp8.h), rows of scale_pitch bytes
+  int scale_pitch;
 };
 
 // How a launch cuts the vocabulary into the tiles' slabs: slabs [0, n_main) of `width` ids, then
@@ -670,6 +673,7 @@ struct TileFamily {
   static constexpr bool STREAM_W = STREAM_W_;
   using MF = MF_;
   using C = LmheadCfg<TV, TR, WV, WR, BK, NST, MF>;
+  static constexpr bool kFp8 = false;
   static_assert(C::kCntOff + 8 <= C::kLds, "epilogue scratch exceeds the LDS ring");
 };
 
@@ -723,10 +727,10 @@ __device__ __forceinline__ TileAt tile_at(const SlabCut& cut, int V, int RT, int
 }
 
 // One tile: ids v0 .. v_end - 1 (at most TV), tree rows r0 .. r0 + TR - 1; `rec` is the record
-// each of its rows writes.
-template <class F>
+// each of its rows writes. E: what is applied to the logits first (NoRules or RuleArgs).
+template <class F, class E>
 __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_end, int r0,
-                                             int rec, uint4* smem) {
+                                             int rec, uint4* smem, const E& rules) {
   constexpr int TR = F::TR, WV = F::WV;
   using MF = typename F::MF;
   using C = typename F::C;
@@ -777,7 +781,11 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
 
   // ---- the tile's logits
   typename MF::Acc acc[C::MV][C::MR];
-  family_tile<F>(X, W, N, H, V, v0, v_end, r0, smem, w_packed, acc);
+  if constexpr (F::kFp8)
+    F::logits(a, v0, v_end, r0, smem, acc);
+  else
+    family_tile<F>(X, W, N, H, V, v0, v_end, r0, smem, w_packed, acc);
+  if constexpr (E::kRules) apply_rules<F>(rules, a, v0, v_end, r0, smem, acc);
 
   // Output block (i, j), register e of a lane holds vocab row kBlock i + MF::row_of(lane, e)
   // (of the wave's vocab range) and tree row kBlock j + lane % kBlock (of the wave's rows).
@@ -963,11 +971,15 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
 }
 
 // A launch of K1: the tiles of cut's slabs x RT row tiles on family M, the tail's on family T.
-template <class M, class T>
+template <class M, class T, class E>
 __global__ __launch_bounds__(M::C::kThreads, 1)
-void k_lmhead_partial(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_rows) {
+void k_lmhead_partial(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_rows, E rules) {
   static_assert(M::C::kThreads == T::C::kThreads, "one workgroup shape");
-  __shared__ uint4 smem[(M::C::kLds > T::C::kLds ? M::C::kLds : T::C::kLds) / 16];
+  constexpr int kLds = M::C::kLds > T::C::kLds ? M::C::kLds : T::C::kLds;
+  constexpr int kTile = E::kRules ? (int)sizeof(RuleTile<M::TR, M::TV>) : 0;
+  constexpr int kTail = E::kRules ? (int)sizeof(RuleTile<T::TR, T::TV>) : 0;
+  constexpr int kBytes = kLds > kTile ? (kLds > kTail ? kLds : kTail) : (kTile > kTail ? kTile : kTail);
+  __shared__ uint4 smem[(kBytes + 15) / 16];
   // clear the per-request completion counters of the finishing kernel that follows
   for (int i = blockIdx.x * M::C::kThreads + threadIdx.x; i < a.n_cnt;
        i += gridDim.x * M::C::kThreads)
@@ -975,9 +987,9 @@ void k_lmhead_partial(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_
   const TileAt t = tile_at(cut, a.V, RT, M::TR == T::TR ? RT : (a.N + T::TR - 1) / T::TR, blk_slabs,
                            blk_rows);
   if constexpr (!std::is_same_v<M, T>) {
-    if (t.tail) return lmhead_block<T>(a, t.v0, t.v_end, t.rt * T::TR, t.rec, smem);
+    if (t.tail) return lmhead_block<T>(a, t.v0, t.v_end, t.rt * T::TR, t.rec, smem, rules);
   }
-  lmhead_block<M>(a, t.v0, t.v_end, t.rt * M::TR, t.rec, smem);
+  lmhead_block<M>(a, t.v0, t.v_end, t.rt * M::TR, t.rec, smem, rules);
 }
 
 // ---- packed weights

@@ -78,7 +78,7 @@ struct ConfShare {
 };
 
 // A launch of its own, one workgroup per share.
-__global__ __launch_bounds__(kConfWaves * kWave)
+static __global__ __launch_bounds__(kConfWaves * kWave)
 void k_draft_conf_partial(ConfArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   ConfShare c;
