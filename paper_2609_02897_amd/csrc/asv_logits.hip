@@ -69,29 +69,35 @@ int round_rows(const uint16_t* hidden, const void* w, int N, int H, int V, char*
 // ---- launches of the 8-bit LM head
 
 using Q8Rows64 = Q8Family<256, 64, 4, 1, 3, 0, true>;
-using Q8Rows128 = Q8Family<256, 128, 2, 2, 4, 0, true>;
-using Q8Rows256 = Q8Family<256, 256, 2, 2, 3, 0, false>;
+using Q8Rows128 = Q8Family<256, 128, 2, 2, 3, 3, true>;
+using Q8Rows192 = Q8Family<256, 192, 2, 2, 3, 3, false>;
+using Q8Rows256 = Q8Family<256, 256, 2, 2, 3, 3, false>;
 
-// f(family tag, tile order) for N rows
+// f(family tag, launch) for the launches of N rows: K1's plan over whole slabs.
 template <class Fn>
-void with_q8_family(int N, int V, int cus, Fn&& f) {
-  asv_k1_launch k{};
-  k.n_slabs = (V + kSlab - 1) / kSlab;
-  k.tile_rows = N <= 64 ? 64 : N <= 128 ? 128 : 256;
-  k.row_tiles = (N + k.tile_rows - 1) / k.tile_rows;
-  tile_blocking(k.row_tiles, cus, &k.blk_slabs, &k.blk_rows);
-  if (N <= 64) f(Q8Rows64{}, k);
-  else if (N <= 128) f(Q8Rows128{}, k);
-  else f(Q8Rows256{}, k);
+void q8_launches(int N, int V, int cus, Fn&& f) {
+  const int S = (V + kSlab - 1) / kSlab;
+  asv_k1_launch k[2];
+  const int n = k1_launches(N, S, cus, plan_k1(N, S, cus), k);
+  for (int q = 0; q < n; ++q) switch (k[q].tile_rows) {
+      case 64: f(Q8Rows64{}, k[q]); break;
+      case 128: f(Q8Rows128{}, k[q]); break;
+      case 192: f(Q8Rows192{}, k[q]); break;
+      default: f(Q8Rows256{}, k[q]); break;
+    }
+}
+
+SlabCut whole_slabs(const asv_k1_launch& k) {
+  return SlabCut{k.n_slabs, kSlab, kSlab, k.slab0, k.slab0 * kSlab};
 }
 
 template <class T>
 void launch_logits(const LmheadArgs& g, const asv_logits_args* a, hipStream_t s) {
-  with_q8_family(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
+  q8_launches(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
     using F = decltype(family);
-    const SlabCut cut{k.n_slabs, kSlab, kSlab, 0, 0};
     k_lmhead_logits<F, T><<<k.n_slabs * k.row_tiles, F::C::kThreads, 0, s>>>(
-        g, cut, k.row_tiles, k.blk_slabs, k.blk_rows, static_cast<T*>(a->out), a->out_pitch);
+        g, whole_slabs(k), k.row_tiles, k.blk_slabs, k.blk_rows, static_cast<T*>(a->out),
+        a->out_pitch);
   });
 }
 
@@ -103,10 +109,8 @@ int verify_fp8(const asv_verify_args* a, char* ws, hipStream_t s, const E& e) {
   LmheadArgs g = lmhead_args(a, L, ws, S);
   if (int rc = round_rows(a->hidden, a->w_lm, a->N, a->H, a->V, ws + L.bytes, s, &g)) return rc;
   if (int rc = draft_conf(a, L, ws, a->N <= 64 ? S : 0, s, &g.conf)) return rc;
-  with_q8_family(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
-    using F = decltype(family);
-    launch_lmhead<F>(g, SlabCut{k.n_slabs, kSlab, kSlab, 0, 0}, 0, k, s,
-                     K1Events{nullptr, nullptr}, e);
+  q8_launches(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
+    launch_lmhead<decltype(family)>(g, whole_slabs(k), 0, k, s, K1Events{nullptr, nullptr}, e);
   });
   if (int rc = launch_status("k_lmhead_partial")) return rc;
   return finish_verify<E::kRules>(a, L, ws, S, s);

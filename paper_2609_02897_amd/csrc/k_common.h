@@ -165,6 +165,15 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// 1, which the compiler takes for any number. Behind a K loop, accumulators that are stored or selected as
+// they are, not computed with, have the loop move them between the register files on every pass
+// (one to two moves a matrix instruction): a product with one keeps them apart.
+__device__ __forceinline__ float opaque_one() {
+  float one = 1.f;
+  asm volatile("" : "+v"(one));
+  return one;
+}
+
 // f(std::integral_constant<int, i>{}) for i = 0 .. M-1, each i a compile-time constant (a
 // fully unrolled loop whose body may select code with if constexpr).
 template <int M, typename F>

@@ -270,11 +270,22 @@ struct Q8Io {
   __device__ __forceinline__ bf16x8 x_frag(int slot, int s, int j) const {
     return __builtin_bit_cast(bf16x8, (lds + slot * (C::kStage / 16) + x_frag0[s])[128 * j]);
   }
-  // the scales of K stage ks: of the wave's first block of ids, and of the next one
+  // the scales of K stage ks, of the wave's first block of ids and of the next one: the words that hold
+  // them, and the scales themselves
+  __device__ __forceinline__ void step_words(int ks, uint32_t& a, uint32_t& b) const {
+    a = wa[ks >> 3];
+    b = wb[ks >> 3];
+  }
+  __device__ __forceinline__ void steps_of(int ks, uint32_t wa_, uint32_t wb_, float& a,
+                                           float& b) const {
+    const int sh = 8 * ((ks >> 1) & 3);
+    a = q8_step((wa_ >> sh) & 255);
+    b = q8_step((wb_ >> sh) & 255);
+  }
   __device__ __forceinline__ void steps(int ks, float& a, float& b) const {
-    const int kb = ks >> 1, sh = 8 * (kb & 3);
-    a = q8_step((wa[kb >> 2] >> sh) & 255);
-    b = q8_step((wb[kb >> 2] >> sh) & 255);
+    uint32_t x, y;
+    step_words(ks, x, y);
+    steps_of(ks, x, y, a, b);
   }
 };
 
@@ -336,6 +347,106 @@ __device__ __forceinline__ void q8_ring(const LmheadArgs& a, int v0, int v_end, 
   __syncthreads();
 }
 
+// Half h of the fragment of matrix step s (four codes).
+template <int s, int h>
+__device__ __forceinline__ void q8_widen_half(const uint4& c, float step, uint32_t (&f)[4]) {
+  const uint32_t x = s == 0 ? (h == 0 ? c.x : c.y) : (h == 0 ? c.z : c.w);
+  f[2 * h] = q8_value_pair<false>(x, step);
+  f[2 * h + 1] = q8_value_pair<true>(x, step);
+}
+
+// The spread K loop in a three-slot ring, one barrier per stage (see lmhead_tile_spread3): copies, LDS
+// reads and widening stand between the matrix instructions, one position m = (s MV + i) MR + j each.
+//   m < MR          the X fragments of step 1 of slot k;
+//   m < Q2          the remaining copies of stage k + 2;
+//   m = Q2 - 1      wait until stage k + 1 has landed (only copies of stage k + 2 may be outstanding) +
+//                   barrier;
+//   m >= Q2         of stage k + 1: the codes of block 0, the X fragments of step 0, the other codes (the
+//                   codes of a block are overwritten after its last widening, which is just
+//                   before they may be); the first copies of stage k + 3.
+// Block i of step s is widened at the last positions of the block before it, into the other of two
+// fragments. Past the last stage the copies repeat the last stage into slots no later stage reads,
+// and what is read of the stage after the last is discarded.
+template <class F>
+__device__ __forceinline__ void q8_spread3(const LmheadArgs& a, int v0, int v_end, int r0,
+                                           uint4* smem, f32x4 (&acc)[F::C::MV][F::C::MR]) {
+  using C = typename F::C;
+  constexpr int NST = 3, MV = C::MV, MR = C::MR, NS = C::NS, NF = MV + MR;
+  constexpr int NM = NS * MV * MR, G = C::kLoads, Q2 = NM - NF;
+  static_assert(F::NST == NST && NS == 2 && MV % 2 == 0 && MR >= 2, "schedule");
+  static_assert(Q2 >= MR + 2 && Q2 >= MV * MR, "reads of a stage end before the next one's");
+  static_assert(2 * G <= 63, "vmcnt range");
+  constexpr auto rel = [](int c) { return c * NM / G; };
+  constexpr int n1 = [&] {
+    int n = 0;
+    for (int c = 0; c < G; ++c) n += Q2 + rel(c) < NM ? 1 : 0;
+    return n;
+  }();
+  const Q8Io<F> io(a, v0, v_end, r0, smem);
+  const int KT = a.H / F::BK;
+  auto issue_copy = [&](int j, auto cc) {
+    io.template copy<decltype(cc)::value>(j % NST, min(j, KT - 1));
+  };
+  zero_acc(acc);
+  uint4 w[MV];
+  bf16x8 x[NS][MR];
+  uint32_t f[2][4];
+
+  static_for<G>([&](auto cc) { issue_copy(0, cc); });
+  static_for<G>([&](auto cc) { issue_copy(1, cc); });
+  static_for<G>([&](auto cc) {
+    if constexpr (decltype(cc)::value < n1) issue_copy(2, cc);
+  });
+  float sa, sb, na, nb;
+  io.steps(0, sa, sb);
+  wait_vm_barrier<G + n1>();
+  static_for<MV>([&](auto ic) { w[decltype(ic)::value] = io.w_codes(0, decltype(ic)::value); });
+  static_for<MR>([&](auto jc) {
+    x[0][decltype(jc)::value] = io.x_frag(0, 0, decltype(jc)::value);
+  });
+  q8_widen_half<0, 0>(w[0], sa, f[0]);
+  q8_widen_half<0, 1>(w[0], sa, f[0]);
+
+  int slot = 0;
+  for (int k = 0; k < KT; ++k) {
+    const int nslot = slot == NST - 1 ? 0 : slot + 1;
+    uint32_t wa = 0, wb = 0;
+    const int kn = min(k + 1, KT - 1);
+    static_for<NM>([&](auto mc) {
+      constexpr int m = decltype(mc)::value;
+      constexpr int s = m / (MV * MR), q = m % (MV * MR), i = q / MR, j = q % MR;
+      constexpr int b = s * MV + i, nb_ = (b + 1) % (NS * MV), ns = nb_ / MV, ni = nb_ % MV;
+      acc[i][j] = Mfma16::mma(
+          __builtin_bit_cast(bf16x8, make_uint4(f[b & 1][0], f[b & 1][1], f[b & 1][2], f[b & 1][3])),
+          x[s][j], acc[i][j]);
+      if constexpr (m == 0) io.step_words(kn, wa, wb);
+      if constexpr (m == NM / 2) io.steps_of(kn, wa, wb, na, nb);
+      if constexpr (j >= MR - 2) {
+        constexpr int h = j - (MR - 2);
+        const float step = b + 1 == NS * MV ? (ni < io.split ? na : nb) : (ni < io.split ? sa : sb);
+        q8_widen_half<ns, h>(w[ni], step, f[(b + 1) & 1]);
+      }
+      if constexpr (m < MR) x[1][m] = io.x_frag(slot, 1, m);
+      static_for<G>([&](auto cc) {
+        constexpr int c = decltype(cc)::value;
+        if constexpr (c >= n1 && Q2 + rel(c) - NM == m) issue_copy(k + 2, cc);
+        if constexpr (c < n1 && Q2 + rel(c) == m) issue_copy(k + 3, cc);
+      });
+      if constexpr (m == Q2 - 1) wait_vm_barrier<G>();
+      if constexpr (m == Q2) w[0] = io.w_codes(nslot, 0);
+      if constexpr (m > Q2 && m <= Q2 + MR) x[0][m - Q2 - 1] = io.x_frag(nslot, 0, m - Q2 - 1);
+      if constexpr (m > Q2 + MR) w[m - Q2 - MR] = io.w_codes(nslot, m - Q2 - MR);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    sa = na;
+    sb = nb;
+    slot = nslot;
+  }
+  // every copy lands before the caller reuses the ring and before the workgroup can exit
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+  __syncthreads();
+}
+
 template <int TV, int TR, int WV, int WR, int NST, int LOOP, bool STREAM_W>
 __device__ __forceinline__ void Q8Family<TV, TR, WV, WR, NST, LOOP, STREAM_W>::logits(
     const LmheadArgs& a, int v0, int v_end, int r0, uint4* smem, f32x4 (&acc)[C::MV][C::MR]) {
@@ -344,7 +455,8 @@ __device__ __forceinline__ void Q8Family<TV, TR, WV, WR, NST, LOOP, STREAM_W>::l
   v0 = __builtin_amdgcn_readfirstlane(v0);
   v_end = __builtin_amdgcn_readfirstlane(v_end);
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  q8_ring<Q8Family>(a, v0, v_end, r0, smem, acc);
+  if constexpr (LOOP == 3) q8_spread3<Q8Family>(a, v0, v_end, r0, smem, acc);
+  else q8_ring<Q8Family>(a, v0, v_end, r0, smem, acc);
 }
 
 // The logits themselves: the tiles of cut's slabs x RT row tiles, rows of `pitch` elements of T.
@@ -363,6 +475,7 @@ void k_lmhead_logits(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_r
   const int wv = wave % F::WV, wr = wave / F::WV;
   typedef T Tv __attribute__((__vector_size__(4 * sizeof(T))));
   const bool wide = pitch % 4 == 0 && reinterpret_cast<uintptr_t>(out) % sizeof(Tv) == 0;
+  const float one = opaque_one();
   static_for<C::MR>([&](auto jc) {
     constexpr int j = decltype(jc)::value;
     const int n = r0 + wr * C::kWaveR + 16 * j + (lane & 15);
@@ -370,16 +483,16 @@ void k_lmhead_logits(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_r
     static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
       const int v = t.v0 + wv * C::kWaveV + 16 * i + 4 * (lane >> 4);
+      Tv x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = (T)(acc[i][j][e] * one);
       if (n >= a.N) return;
       if (wide && v + 4 <= t.v_end) {
-        Tv x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (T)acc[i][j][e];
         *reinterpret_cast<Tv*>(row + v) = x;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (v + e < t.v_end) row[v + e] = (T)acc[i][j][e];
+          if (v + e < t.v_end) row[v + e] = x[e];
       }
     });
     __builtin_amdgcn_sched_barrier(0);

@@ -769,6 +769,11 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     }
   }
 
+  RowRule my_rule{};                   // of request tid, for the rules
+  if constexpr (E::kRules) {
+    if (tid < B) my_rule = row_rule(rules, tid);
+  }
+
   // ---- the tile's share of the draft logits, loaded here and reduced at the end. 64-row tiles
   // only: the larger ones have no registers to keep it in (loaded after the K loop instead, the
   // 256-row tile spilled: 3048 rows 2779 -> 2893 us, 190 and 378 rows level).
@@ -785,7 +790,14 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     F::logits(a, v0, v_end, r0, smem, acc);
   else
     family_tile<F>(X, W, N, H, V, v0, v_end, r0, smem, w_packed, acc);
-  if constexpr (E::kRules) apply_rules<F>(rules, a, v0, v_end, r0, smem, acc);
+  struct Nothing {
+    __device__ Nothing(const E&, const LmheadArgs&, int, int, int, void*, int) {}
+  };
+  using Ruled = std::conditional_t<E::kRules, TileRules<F>, Nothing>;
+  Ruled ruled(rules, a, v0, v_end, r0, smem, [&] {
+    if constexpr (E::kRules) return RulePrefetch<C::kCand>{off_lo, off_hi, my_rule, cc, cp, cd};
+    else return 0;
+  }());
 
   // Output block (i, j), register e of a lane holds vocab row kBlock i + MF::row_of(lane, e)
   // (of the wave's vocab range) and tree row kBlock j + lane % kBlock (of the wave's rows).
@@ -795,10 +807,14 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
   int4* const s_list = reinterpret_cast<int4*>(lds_bytes);
   float* const wscr =
       reinterpret_cast<float*>(lds_bytes + C::kScrOff) + wave * (kWave * kRegs);
-  float* const red_m = reinterpret_cast<float*>(lds_bytes + C::kRedOff);
+  constexpr int kRedOff = [] {
+    if constexpr (E::kRules) return TileRules<F>::kRedOff;
+    else return C::kRedOff;
+  }();
+  float* const red_m = reinterpret_cast<float*>(lds_bytes + kRedOff);
   float* const red_s = red_m + WV * TR;
   int* const red_a = reinterpret_cast<int*>(red_s + WV * TR);
-  int* const s_seg_end = reinterpret_cast<int*>(lds_bytes + C::kCntOff);
+  int* const s_seg_end = reinterpret_cast<int*>(lds_bytes + kRedOff + (C::kCntOff - C::kRedOff));
   int* const s_cnt = s_seg_end + 1;
 
   // ---- drafted logits: nodes whose parent row and drafted token fall inside this tile.
@@ -862,7 +878,11 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
             for (int e2 = 0; e2 < kRegs; ++e2) wscr[e2 * kWave + lane] = acc[i][j][e2];
           }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
-      if (lane == owner) drafted_logit[m.x] = wscr[ee * kWave + owner];
+      if (lane == owner) {
+        float z = wscr[ee * kWave + owner];
+        if constexpr (E::kRules) z = ruled.one(m.y, m.z, z);
+        drafted_logit[m.x] = z;
+      }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     }
     __syncthreads();
@@ -887,11 +907,29 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
   };
   constexpr int kEntries = C::MV * kRegs;
   static_assert(kEntries % 4 == 0, "entries in groups of four");
+  [[maybe_unused]] auto held = [&] {
+    if constexpr (E::kRules) {
+      ruled.fill_paths();
+      typename Ruled::Held h;
+      ruled.begin(h);
+      return h;
+    } else
+      return 0;
+  }();
   // Branch-free record of row block j over the wave's ids; MASK drops entries past v_end.
   auto row_record = [&](int j, auto mask_tag) -> Rec {
     constexpr bool MASK = decltype(mask_tag)::value;
+    float zr[E::kRules ? kEntries : 1];
+    if constexpr (E::kRules) {
+      typename MF::Acc col[C::MV];
+#pragma unroll
+      for (int i = 0; i < C::MV; ++i) col[i] = acc[i][j];
+      ruled.block(j, col, zr, held);
+    }
     auto entry = [&](int k) {
-      const float z = acc[k / kRegs][j][k % kRegs];
+      float z;
+      if constexpr (E::kRules) z = zr[k];
+      else z = acc[k / kRegs][j][k % kRegs];
       if constexpr (MASK) return entry_v(k) < v_end ? z : kNegInf;
       else return z;
     };
@@ -942,8 +980,7 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     a = min((int)lo, (int)hi);
     return Rec{m, m == kNegInf ? 0.f : sum, m == kNegInf ? kNoIndex : a};
   };
-#pragma unroll
-  for (int j = 0; j < C::MR; ++j) {
+  auto write_record = [&](int j) {
     const Rec r = full ? row_record(j, std::false_type{}) : row_record(j, std::true_type{});
     if (lane < kBlock) {
       const int row = wr * C::kWaveR + kBlock * j + lane;
@@ -952,6 +989,12 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
       red_a[wv * TR + row] = r.a;
     }
     __builtin_amdgcn_sched_barrier(0);
+  };
+  if constexpr (E::kRules) {
+    static_for<C::MR>([&](auto jc) { write_record(decltype(jc)::value); });
+  } else {
+#pragma unroll
+    for (int j = 0; j < C::MR; ++j) write_record(j);
   }
   __syncthreads();
   for (int row = tid; row < TR; row += T) {
@@ -970,16 +1013,28 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
   if constexpr (TR == 64) conf.finish(a.conf, lane);
 }
 
+// LDS of a launch of K1. The rules' registers must not cost the second workgroup of a CU that the ring
+// leaves room for.
+template <class M, class T, class E>
+constexpr int lmhead_lds() {
+  int n = M::C::kLds > T::C::kLds ? M::C::kLds : T::C::kLds;
+  if constexpr (E::kRules) {
+    n = n > TileRules<M>::kBytes ? n : TileRules<M>::kBytes;
+    n = n > TileRules<T>::kBytes ? n : TileRules<T>::kBytes;
+  }
+  return n;
+}
+template <class M, class T, class E>
+constexpr int lmhead_waves() {
+  return E::kRules && lmhead_lds<M, T, E>() <= 80 * 1024 ? 2 : 1;
+}
+
 // A launch of K1: the tiles of cut's slabs x RT row tiles on family M, the tail's on family T.
 template <class M, class T, class E>
-__global__ __launch_bounds__(M::C::kThreads, 1)
+__global__ __launch_bounds__(M::C::kThreads, (lmhead_waves<M, T, E>()))
 void k_lmhead_partial(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_rows, E rules) {
   static_assert(M::C::kThreads == T::C::kThreads, "one workgroup shape");
-  constexpr int kLds = M::C::kLds > T::C::kLds ? M::C::kLds : T::C::kLds;
-  constexpr int kTile = E::kRules ? (int)sizeof(RuleTile<M::TR, M::TV>) : 0;
-  constexpr int kTail = E::kRules ? (int)sizeof(RuleTile<T::TR, T::TV>) : 0;
-  constexpr int kBytes = kLds > kTile ? (kLds > kTail ? kLds : kTail) : (kTile > kTail ? kTile : kTail);
-  __shared__ uint4 smem[(kBytes + 15) / 16];
+  __shared__ uint4 smem[(lmhead_lds<M, T, E>() + 15) / 16];
   // clear the per-request completion counters of the finishing kernel that follows
   for (int i = blockIdx.x * M::C::kThreads + threadIdx.x; i < a.n_cnt;
        i += gridDim.x * M::C::kThreads)

@@ -7,7 +7,7 @@
 //   z3 = z2 + bias[v]
 //   z4 = allowed[n][v] ? z3 : -inf
 // K10 k_token_counts: the history table from token lists. K11 k_adjust: the rules on logits in
-// memory. apply_rules: the rules on a tile of logits in the accumulators of the LM-head kernel.
+// memory. TileRules: the rules on a tile of logits in the accumulators of the LM-head kernel.
 #pragma once
 
 #include "asv.h"
@@ -39,9 +39,10 @@ struct RowRule {
 
 // A logit under its row's penalties: table entry c, drafted `path` times on the row's path.
 __device__ __forceinline__ float penalised(float z, int c, int path, const RowRule& r) {
+  // (rounded operation by operation: a token's logit is the same wherever it is computed)
   const int g = (c & kCountMask) + path;
-  if (c != 0 || path != 0) z = z > 0.f ? z / r.rep : z * r.rep;
-  if (g > 0) z -= fmaf(r.freq, (float)g, r.pres);
+  if (c != 0 || path != 0) z = z > 0.f ? z / r.rep : __fmul_rn(z, r.rep);
+  if (g > 0) z = __fsub_rn(z, __fmaf_rn(r.freq, (float)g, r.pres));
   return z;
 }
 
@@ -51,6 +52,27 @@ __device__ __forceinline__ float penalised(float z, int c, int path, const RowRu
 // whether one of these nodes drafted one of the ids v0 .. v_end - 1.
 constexpr int kPathStage = 512;      // nodes whose links and tokens are walked in LDS
 
+__device__ __forceinline__ RowRule row_rule(const RuleArgs& a, int b) {
+  return RowRule{a.repetition ? a.repetition[b] : 1.f, a.presence ? a.presence[b] : 0.f,
+                 a.frequency ? a.frequency[b] : 0.f};
+}
+
+// What a thread may have loaded before RuleRows::build: the offsets and penalties of request threadIdx.x
+// (where there is one), and nodes c = r0 + 1 + k T + threadIdx.x with their links and tokens.
+struct NoPrefetch {
+  static constexpr bool kHas = false;
+  int lo, hi;
+  RowRule rule;
+};
+template <int CAND>
+struct RulePrefetch {
+  static constexpr bool kHas = true;
+  static constexpr int kCand = CAND;
+  int lo, hi;
+  RowRule rule;
+  const int *c, *p, *d;
+};
+
 template <int TR>
 struct RuleRows {
   int req[TR], lo[TR];
@@ -58,17 +80,14 @@ struct RuleRows {
   int seg_lo, hit;
   int tok[kPathStage], par[kPathStage];
 
-  // All threads of the workgroup, T of them; draft_tok null: no paths, off null: row n is request n.
-  template <int T>
+  // All threads of the workgroup, T of them; draft_tok null: no paths, off null: row n is request n. `pre`:
+  // what the thread has loaded beforehand (NoPrefetch: nothing).
+  template <int T, class P>
   __device__ __forceinline__ void build(const RuleArgs& a, const int32_t* __restrict__ off,
                                         const int32_t* __restrict__ parent,
                                         const int32_t* __restrict__ draft_tok, int B, int N,
-                                        int r0, int v0, int v_end) {
+                                        int r0, int v0, int v_end, const P& pre) {
     const int tid = threadIdx.x, r_end = min(r0 + TR, N);
-    auto row_rule = [&](int b) {
-      return RowRule{a.repetition ? a.repetition[b] : 1.f, a.presence ? a.presence[b] : 0.f,
-                     a.frequency ? a.frequency[b] : 0.f};
-    };
     if (tid == 0) {
       seg_lo = r0;
       hit = 0;
@@ -76,7 +95,7 @@ struct RuleRows {
     if (!off) {
       for (int i = tid; r0 + i < r_end; i += T) {
         req[i] = r0 + i;
-        rule[i] = row_rule(r0 + i);
+        rule[i] = row_rule(a, r0 + i);
       }
       __syncthreads();
       return;
@@ -87,9 +106,11 @@ struct RuleRows {
     }
     __syncthreads();
     for (int b = tid; b < B; b += T) {
-      const int first = off[b], from = max(first, r0), to = min(off[b + 1], r_end);
+      const bool known = P::kHas && b == tid;
+      const int first = known ? pre.lo : off[b];
+      const int from = max(first, r0), to = min(known ? pre.hi : off[b + 1], r_end);
       if (first < 0 || from >= to) continue;
-      const RowRule r = row_rule(b);
+      const RowRule r = known ? pre.rule : row_rule(a, b);
       for (int n = from; n < to; ++n) {
         req[n - r0] = b;
         lo[n - r0] = first;
@@ -101,13 +122,23 @@ struct RuleRows {
     if (!draft_tok) return;
     const int base = seg_lo;
     bool any = false;
-    for (int c = base + tid; c < r_end; c += T) {
-      const int d = draft_tok[c];
+    auto put = [&](int c, int p, int d) {
       any |= d >= v0 && d < v_end;
       if (c - base < kPathStage) {
         tok[c - base] = d;
-        par[c - base] = parent[c];
+        par[c - base] = p;
       }
+    };
+    if constexpr (P::kHas) {
+      // nodes r0 + 1 .. of the rows are known; r0 is a root where no request starts before it
+      static_assert(P::kCand * T >= TR, "every row's node is prefetched");
+#pragma unroll
+      for (int k = 0; k < P::kCand; ++k)
+        if (pre.c[k] < r_end) put(pre.c[k], pre.p[k], pre.d[k]);
+      if (base < r0)
+        for (int c = base + tid; c <= r0; c += T) put(c, parent[c], draft_tok[c]);
+    } else {
+      for (int c = base + tid; c < r_end; c += T) put(c, parent[c], draft_tok[c]);
     }
     if (any) hit = 1;
     __syncthreads();
@@ -130,16 +161,6 @@ struct RuleRows {
   }
 };
 
-// The same for a tile of the LM-head kernel, with how often each row's path drafted each of the
-// tile's ids, filled only where `hit`: 16 bits hold any path of so many rows.
-constexpr int kMaxRuledRows = 65535;
-
-template <int TR, int TV>
-struct RuleTile {
-  RuleRows<TR> rows;
-  uint16_t path[TR][TV];
-};
-
 // Four consecutive entries of a [..][V] row from id v on (a multiple of 4), 0 past V.
 template <class T4, class T>
 __device__ __forceinline__ T4 load4(const T* __restrict__ row, int v, int V, bool wide) {
@@ -157,90 +178,158 @@ __device__ __forceinline__ T4 load4(const T* __restrict__ row, int v, int V, boo
 typedef int i32x4 __attribute__((__vector_size__(16)));
 typedef float fx4 __attribute__((__vector_size__(16)));
 
-// The rules on one tile of the LM-head kernel, in its accumulators. Every tile reads its ids' slice
-// of the table, the bias and the mask once per 16 rows, through the caches: with one request that is
-// 9 bytes an id beside the weight's 2 H. The loads of a row block are issued together.
-template <class F, class A>
-__device__ __forceinline__ void apply_rules(const RuleArgs& r, const A& a, int v0, int v_end, int r0,
-                                            void* smem,
-                                            typename F::MF::Acc (&acc)[F::C::MV][F::C::MR]) {
+// The rules on one tile of the LM-head kernel. Its accumulators are only read: the drafted logits' gather
+// (`one`) and the record of a row block (`block`) take each logit through the rules on its way, since a
+// loop whose accumulators are changed behind it has them moved between register files on every pass.
+// Every tile reads its ids' slice of the table, the bias and the mask once per 16 rows, through the caches:
+// with one request 9 bytes an id beside the weight's H or 2 H.
+//
+// LDS: how often each row's path drafted each of the tile's ids, filled only where `hit` (16 bits hold
+// any path of kMaxRuledRows rows); over it, before it is filled, the gather's list and scratch; behind
+// it the record exchange, the counters and the rows.
+constexpr int kMaxRuledRows = 65535;
+
+template <class F>
+struct TileRules {
   using C = typename F::C;
+  using Rows = RuleRows<F::TR>;
+  static constexpr int kPath = F::TR * F::TV * 2;
+  static constexpr int kRedOff = (kPath > C::kRedOff ? kPath : C::kRedOff);
+  static constexpr int kCntOff = kRedOff + (C::kCntOff - C::kRedOff);
+  static constexpr int kRowsOff = (kCntOff + 8 + 15) / 16 * 16;
+  static constexpr int kBytes = kRowsOff + (int)sizeof(Rows);
   static_assert(F::MF::kBlock == 16 && F::MF::kRegs == 4, "four consecutive ids a lane and block");
-  constexpr int T = C::kThreads;
-  auto& tile = *reinterpret_cast<RuleTile<F::TR, F::TV>*>(smem);
-  auto& rows = tile.rows;
-  rows.template build<T>(r, a.req_offsets, a.parent, a.draft_tok, a.B, a.N, r0, v0, v_end);
-  const bool hit = __builtin_amdgcn_readfirstlane(rows.hit);
-  if (hit) {
-    uint32_t* words = reinterpret_cast<uint32_t*>(tile.path);
-    for (int i = threadIdx.x; i < F::TR * F::TV / 2; i += T) words[i] = 0;
+  const RuleArgs& r;
+  const int32_t* parent;
+  const int32_t* draft_tok;
+  int N, V, v0, v_end, r0, lane, wr, vw;
+  uint16_t* path;
+  Rows& rows;
+  bool hit, wide_c, wide_b;
+  float unit;
+
+  template <class A, class P>
+  __device__ __forceinline__ TileRules(const RuleArgs& r_, const A& a, int v0_, int v_end_, int r0_,
+                                       void* smem, const P& pre)
+      : r(r_), parent(a.parent), draft_tok(a.draft_tok), N(a.N), V(a.V), v0(v0_), v_end(v_end_),
+        r0(r0_), path(static_cast<uint16_t*>(smem)),
+        rows(*reinterpret_cast<Rows*>(static_cast<char*>(smem) + kRowsOff)) {
+    rows.template build<C::kThreads>(r, a.req_offsets, parent, draft_tok, a.B, N, r0, v0, v_end, pre);
+    hit = __builtin_amdgcn_readfirstlane(rows.hit);
+    unit = opaque_one();
+    lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wr = wave / F::WV;
+    vw = (wave % F::WV) * C::kWaveV + 4 * (lane >> 4);    // this lane's ids of block 0, from v0
+    wide_c = (V & 3) == 0 && (reinterpret_cast<uintptr_t>(r.counts) & 15) == 0;
+    wide_b = (r.bias_pitch & 3) == 0 && (V & 3) == 0 &&
+             (reinterpret_cast<uintptr_t>(r.bias) & 15) == 0;
+  }
+
+  // The logit z of id v0 + dv in row r0 + i, for one lane.
+  __device__ __forceinline__ float one(int i, int dv, float z) const {
+    const int b = rows.req[i], v = v0 + dv;
+    if (b < 0) return z;
+    int n = 0;
+    rows.walk(i, r0, parent, draft_tok, [&](int d) { n += d == v; });
+    z = penalised(z, r.counts ? r.counts[(size_t)b * V + v] : 0, n, rows.rule[i]);
+    if (r.bias) z = __fadd_rn(z, r.bias[(size_t)b * r.bias_pitch + v]);
+    if (r.allowed && !((r.allowed[(size_t)(r0 + i) * r.words + (v >> 5)] >> (v & 31)) & 1))
+      z = kNegInf;
+    return z;
+  }
+
+  // Between the gather and the first block, by every thread.
+  __device__ __forceinline__ void fill_paths() {
+    if (!hit) return;
+    constexpr int T = C::kThreads;
+    uint32_t* words = reinterpret_cast<uint32_t*>(path);
+    for (int i = threadIdx.x; i < kPath / 4; i += T) words[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < min(F::TR, a.N - r0); i += T)
-      rows.walk(i, r0, a.parent, a.draft_tok, [&](int d) {
-        if (d >= v0 && d < v_end) ++tile.path[i][d - v0];
+    for (int i = threadIdx.x; i < min(F::TR, N - r0); i += T)
+      rows.walk(i, r0, parent, draft_tok, [&](int d) {
+        if (d >= v0 && d < v_end) ++path[i * F::TV + d - v0];
       });
     __syncthreads();
   }
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wv = wave % F::WV, wr = wave / F::WV;
-  const int V = a.V;
-  const bool wide_c = (V & 3) == 0 && (reinterpret_cast<uintptr_t>(r.counts) & 15) == 0;
-  const bool wide_b = (r.bias_pitch & 3) == 0 && (V & 3) == 0 &&
-                      (reinterpret_cast<uintptr_t>(r.bias) & 15) == 0;
-  const int vw = wv * C::kWaveV + 4 * (lane >> 4);    // this lane's ids of block 0, from v0
-  constexpr int G = C::MV % 4 == 0 ? 4 : C::MV % 3 == 0 ? 3 : C::MV % 2 == 0 ? 2 : 1;   // blocks whose
-                                                                     // loads are issued together
-  static_for<C::MR * (C::MV / G)>([&](auto jc) {
-    constexpr int j = decltype(jc)::value / (C::MV / G), i0 = decltype(jc)::value % (C::MV / G) * G;
-    const int i_row = wr * C::kWaveR + 16 * j + (lane & 15), n = r0 + i_row;
+
+  // What a lane holds of the table and the bias for its ids, for the request of its last row, and of the
+  // mask for its next row: the rows of a block mostly belong to one request, the block before's, and
+  // the mask's words are on their way while a block is computed.
+  struct Held {
+    int b = -1;
+    i32x4 c[C::MV];
+    fx4 bias[C::MV];
+    uint32_t bits[C::MV];
+  };
+  __device__ __forceinline__ void load_bits(int j, uint32_t (&bits)[C::MV]) const {
+    const int i_row = wr * C::kWaveR + 16 * j + (lane & 15);
+    const bool on = rows.req[i_row] >= 0;
+    static_for<C::MV>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      const int v = v0 + vw + 16 * i;
+      bits[i] = ~0u;
+      if (r.allowed && on && v < v_end)
+        bits[i] = r.allowed[(size_t)(r0 + i_row) * r.words + (v >> 5)] >> (v & 31);
+    });
+  }
+  __device__ __forceinline__ void begin(Held& h) const {
+    static_for<C::MV>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
+      h.c[i] = i32x4{};
+      h.bias[i] = fx4{};
+    });
+    load_bits(0, h.bits);
+  }
+
+  // z[4 i + e]: the ruled logits of row block j, acc[i][e]; blocks in order, begin() before the first.
+  __device__ __forceinline__ void block(int j, const typename F::MF::Acc (&acc)[C::MV],
+                                        float (&z)[4 * C::MV], Held& h) const {
+    const int i_row = wr * C::kWaveR + 16 * j + (lane & 15);
     const int b = rows.req[i_row];
     const bool on = b >= 0;
+    if (!__all(b == h.b)) {
+      static_for<C::MV>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        const int v = v0 + vw + 16 * i;
+        h.c[i] = i32x4{};
+        h.bias[i] = fx4{};
+        if (on && v < v_end) {
+          if (r.counts) h.c[i] = load4<i32x4>(r.counts + (size_t)b * V, v, V, wide_c);
+          if (r.bias) h.bias[i] = load4<fx4>(r.bias + (size_t)b * r.bias_pitch, v, V, wide_b);
+        }
+      });
+      h.b = b;
+    }
     const RowRule rr = rows.rule[i_row];
-    i32x4 c[G];
-    fx4 bias[G];
-    uint32_t bits[G];
-    static_for<G>([&](auto ic) {
+    uint32_t bits[C::MV];
+    static_for<C::MV>([&](auto ic) { bits[decltype(ic)::value] = h.bits[decltype(ic)::value]; });
+    if (j + 1 < C::MR) load_bits(j + 1, h.bits);
+    static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
-      const int v = v0 + vw + 16 * (i0 + i);
-      c[i] = i32x4{};
-      bias[i] = fx4{};
-      bits[i] = ~0u;
-      if (on && v < v_end) {
-        if (r.counts) c[i] = load4<i32x4>(r.counts + (size_t)b * V, v, V, wide_c);
-        if (r.bias) bias[i] = load4<fx4>(r.bias + (size_t)b * r.bias_pitch, v, V, wide_b);
-        if (r.allowed) bits[i] = r.allowed[(size_t)n * r.words + (v >> 5)] >> (v & 31);
-      }
-    });
-    static_for<G>([&](auto ic) {
-      constexpr int i = decltype(ic)::value;
-      const int vl = vw + 16 * (i0 + i);
-      const uint2 p4 = hit && on ? *reinterpret_cast<const uint2*>(&tile.path[i_row][vl])
-                                 : make_uint2(0u, 0u);
-      const bool special =
-          !__all((c[i][0] | c[i][1] | c[i][2] | c[i][3] | (int)(p4.x | p4.y)) == 0);
-      fx4 z = acc[i0 + i][j];
+      const uint2 p4 = hit && on
+                           ? *reinterpret_cast<const uint2*>(&path[i_row * F::TV + vw + 16 * i])
+                           : make_uint2(0u, 0u);
+      const i32x4 c = h.c[i];
+      const bool special = !__all((c[0] | c[1] | c[2] | c[3] | (int)(p4.x | p4.y)) == 0);
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = __fmul_rn(acc[i][e], unit);
       if (special) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int path = ((e < 2 ? p4.x : p4.y) >> (16 * (e & 1))) & 0xffff;
-          z[e] = penalised(z[e], c[i][e], path, rr);
+          const int n_path = ((e < 2 ? p4.x : p4.y) >> (16 * (e & 1))) & 0xffff;
+          y[e] = penalised(y[e], c[e], n_path, rr);
         }
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (r.bias) z[e] += bias[i][e];
-        z[e] = (bits[i] >> e) & 1 ? z[e] : kNegInf;
+        if (r.bias) y[e] = __fadd_rn(y[e], h.bias[i][e]);
+        z[4 * i + e] = (bits[i] >> e) & 1 ? y[e] : kNegInf;
       }
-      // back into the accumulator registers: left to itself the compiler keeps every value that it has
-      // changed in vector registers, and spills
-      asm volatile("" : "+a"(z));
-      acc[i0 + i][j] = z;
-      __builtin_amdgcn_sched_barrier(0);
     });
-  });
-  __syncthreads();
-}
+  }
+};
 
 // ---- the rules on logits in memory (K11)
 
@@ -275,7 +364,8 @@ void k_adjust(AdjustArgs a) {
   const int chunks = (a.V + kIds - 1) / kIds, group = blockIdx.x / chunks;
   const int tid = threadIdx.x, r0 = group * kAdjRows, v0 = (blockIdx.x - group * chunks) * kIds;
   const int v_end = min(v0 + kIds, a.V), r_end = min(r0 + kAdjRows, a.N);
-  rows.template build<kAdjThreads>(a.r, a.off, a.parent, a.draft_tok, a.B, a.N, r0, v0, v_end);
+  rows.template build<kAdjThreads>(a.r, a.off, a.parent, a.draft_tok, a.B, a.N, r0, v0, v_end,
+                                   NoPrefetch{});
   const bool hit = __builtin_amdgcn_readfirstlane(rows.hit);
   const int v = v0 + tid * PT;
   if (v >= v_end) return;
@@ -334,7 +424,7 @@ void k_adjust(AdjustArgs a) {
 #pragma unroll
       for (int e = 0; e < PT; ++e) {
         if (c[e] != 0 || path[e] != 0) z[e] = penalised(z[e], c[e], path[e], rr);
-        if (r.bias) z[e] += bias[e];
+        if (r.bias) z[e] = __fadd_rn(z[e], bias[e]);
         z[e] = (bits >> e) & 1 ? z[e] : kNegInf;
       }
     }
