@@ -799,6 +799,17 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     else return 0;
   }());
 
+  // the gather covers the first loads of the rules, except where the accumulators leave no registers
+  constexpr bool kBeginEarly = C::MV * C::MR < 64;
+  [[maybe_unused]] auto held = [&] {
+    if constexpr (E::kRules) {
+      typename Ruled::Held h;
+      if constexpr (kBeginEarly) ruled.begin(h);
+      return h;
+    } else
+      return 0;
+  }();
+
   // Output block (i, j), register e of a lane holds vocab row kBlock i + MF::row_of(lane, e)
   // (of the wave's vocab range) and tree row kBlock j + lane % kBlock (of the wave's rows).
 
@@ -879,13 +890,20 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
           }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
       if (lane == owner) {
-        float z = wscr[ee * kWave + owner];
-        if constexpr (E::kRules) z = ruled.one(m.y, m.z, z);
-        drafted_logit[m.x] = z;
+        const float z = wscr[ee * kWave + owner];
+        if constexpr (E::kRules) s_list[e].w = __float_as_int(z);
+        else drafted_logit[m.x] = z;
       }
       __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     }
     __syncthreads();
+    if constexpr (E::kRules) {
+      for (int e = tid; e < cnt; e += T) {
+        const int4 m = s_list[e];
+        drafted_logit[m.x] = ruled.one(m.y, m.z, __int_as_float(m.w));
+      }
+      __syncthreads();
+    }
   }
 
   // ---- per-row slab record: the maximum of the wave's entries of a tree row first (lane-local,
@@ -907,25 +925,15 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
   };
   constexpr int kEntries = C::MV * kRegs;
   static_assert(kEntries % 4 == 0, "entries in groups of four");
-  [[maybe_unused]] auto held = [&] {
-    if constexpr (E::kRules) {
-      ruled.fill_paths();
-      typename Ruled::Held h;
-      ruled.begin(h);
-      return h;
-    } else
-      return 0;
-  }();
+  if constexpr (E::kRules) {
+    ruled.find_paths();
+    if constexpr (!kBeginEarly) ruled.begin(held);
+  }
   // Branch-free record of row block j over the wave's ids; MASK drops entries past v_end.
   auto row_record = [&](int j, auto mask_tag) -> Rec {
     constexpr bool MASK = decltype(mask_tag)::value;
-    float zr[E::kRules ? kEntries : 1];
-    if constexpr (E::kRules) {
-      typename MF::Acc col[C::MV];
-#pragma unroll
-      for (int i = 0; i < C::MV; ++i) col[i] = acc[i][j];
-      ruled.block(j, col, zr, held);
-    }
+    [[maybe_unused]] float zr[E::kRules ? kEntries : 1];
+    if constexpr (E::kRules) ruled.block(j, zr, held);
     auto entry = [&](int k) {
       float z;
       if constexpr (E::kRules) z = zr[k];
@@ -981,7 +989,9 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     return Rec{m, m == kNegInf ? 0.f : sum, m == kNegInf ? kNoIndex : a};
   };
   auto write_record = [&](int j) {
-    const Rec r = full ? row_record(j, std::false_type{}) : row_record(j, std::true_type{});
+    Rec r;
+    if constexpr (E::kRules) r = row_record(j, std::false_type{});     // masked by the rules
+    else r = full ? row_record(j, std::false_type{}) : row_record(j, std::true_type{});
     if (lane < kBlock) {
       const int row = wr * C::kWaveR + kBlock * j + lane;
       red_m[wv * TR + row] = r.m;
@@ -991,7 +1001,26 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     __builtin_amdgcn_sched_barrier(0);
   };
   if constexpr (E::kRules) {
-    static_for<C::MR>([&](auto jc) { write_record(decltype(jc)::value); });
+    constexpr int G = Ruled::kStep;
+#pragma unroll 1
+    for (int j = 0; j < C::MR; ++j) {
+      static_for<C::MR / G>([&](auto gc) {          // every G blocks the next G are staged
+        constexpr int j0 = decltype(gc)::value * G;
+        if (j == j0) {
+          const float one = opaque_one();
+          static_for<G * C::MV>([&](auto m) {
+            constexpr int jj = j0 + decltype(m)::value / C::MV, i = decltype(m)::value % C::MV;
+            fx4 z;
+#pragma unroll
+            for (int e = 0; e < kRegs; ++e) z[e] = __fmul_rn(acc[i][jj][e], one);
+            ruled.staged(jj)[i * kWave + lane] = z;
+          });
+          wave_lds_sync();
+        }
+      });
+      if ((ruled.paths >> j) & 1) ruled.fill_paths(j);
+      write_record(j);
+    }
   } else {
 #pragma unroll
     for (int j = 0; j < C::MR; ++j) write_record(j);

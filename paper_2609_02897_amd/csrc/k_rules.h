@@ -34,27 +34,28 @@ struct RuleArgs {
 };
 
 struct RowRule {
-  float rep, pres, freq;
+  float rep, inv, pres, freq;        // inv = 1 / rep: a quotient z / rep is z inv, one rounding more
 };
 
-// A logit under its row's penalties: table entry c, drafted `path` times on the row's path.
+// A logit under its row's penalties: table entry c, drafted `path` times on the row's path. Rounded
+// operation by operation: a token's logit is the same wherever it is computed.
 __device__ __forceinline__ float penalised(float z, int c, int path, const RowRule& r) {
-  // (rounded operation by operation: a token's logit is the same wherever it is computed)
   const int g = (c & kCountMask) + path;
-  if (c != 0 || path != 0) z = z > 0.f ? z / r.rep : __fmul_rn(z, r.rep);
-  if (g > 0) z = __fsub_rn(z, __fmaf_rn(r.freq, (float)g, r.pres));
-  return z;
+  const float scaled = __fmul_rn(z, z > 0.f ? r.inv : r.rep);
+  z = (c | path) != 0 ? scaled : z;
+  const float less = __fsub_rn(z, __fmaf_rn(r.freq, (float)g, r.pres));
+  return g > 0 ? less : z;
 }
 
 // What the rows r0 .. r0 + TR - 1 need, in LDS: each row's request (-1: none, no rules) with its
 // penalties, and the links and tokens of the nodes up to the last row, from the first row's root on.
 // A path is a few tokens out of V, so most workgroups have none of their ids on any path: `hit` says
 // whether one of these nodes drafted one of the ids v0 .. v_end - 1.
-constexpr int kPathStage = 512;      // nodes whose links and tokens are walked in LDS
+constexpr int kPathStage = 256;      // nodes whose links and tokens are walked in LDS
 
 __device__ __forceinline__ RowRule row_rule(const RuleArgs& a, int b) {
-  return RowRule{a.repetition ? a.repetition[b] : 1.f, a.presence ? a.presence[b] : 0.f,
-                 a.frequency ? a.frequency[b] : 0.f};
+  return RowRule{a.repetition ? a.repetition[b] : 1.f, 0.f, a.presence ? a.presence[b] : 0.f,
+                 a.frequency ? a.frequency[b] : 0.f};     // inv: see RuleRows::put_rule
 }
 
 // What a thread may have loaded before RuleRows::build: the offsets and penalties of request threadIdx.x
@@ -75,8 +76,8 @@ struct RulePrefetch {
 
 template <int TR>
 struct RuleRows {
-  int req[TR], lo[TR];
-  RowRule rule[TR];
+  int2 at[TR];                 // request and its first row
+  RowRule rules[TR];           // of the request that starts, or goes on, at this row
   int seg_lo, hit;
   int tok[kPathStage], par[kPathStage];
 
@@ -94,28 +95,21 @@ struct RuleRows {
     }
     if (!off) {
       for (int i = tid; r0 + i < r_end; i += T) {
-        req[i] = r0 + i;
-        rule[i] = row_rule(a, r0 + i);
+        at[i] = make_int2(r0 + i, r0 + i);
+        put_rule(i, row_rule(a, r0 + i));
       }
       __syncthreads();
       return;
     }
-    for (int i = tid; i < TR; i += T) {
-      req[i] = -1;
-      lo[i] = 0;
-    }
+    for (int i = tid; i < TR; i += T) at[i] = make_int2(-1, r0);
     __syncthreads();
     for (int b = tid; b < B; b += T) {
       const bool known = P::kHas && b == tid;
       const int first = known ? pre.lo : off[b];
       const int from = max(first, r0), to = min(known ? pre.hi : off[b + 1], r_end);
       if (first < 0 || from >= to) continue;
-      const RowRule r = known ? pre.rule : row_rule(a, b);
-      for (int n = from; n < to; ++n) {
-        req[n - r0] = b;
-        lo[n - r0] = first;
-        rule[n - r0] = r;
-      }
+      put_rule(from - r0, known ? pre.rule : row_rule(a, b));
+      for (int n = from; n < to; ++n) at[n - r0] = make_int2(b, first);
       if (first < r0) seg_lo = first;         // the one request that starts before the rows
     }
     __syncthreads();
@@ -144,13 +138,22 @@ struct RuleRows {
     __syncthreads();
   }
 
+  __device__ __forceinline__ void put_rule(int i, RowRule r) {
+    r.inv = 1.f / r.rep;
+    rules[i] = r;
+  }
+  __device__ __forceinline__ int req(int i) const { return at[i].x; }
+  __device__ __forceinline__ const RowRule& rule(int i, int r0) const {
+    return rules[max(at[i].y, r0) - r0];
+  }
+
   // f(token) for the nodes on the path of row r0 + i, from node r0 + i up, the root left out. A link that
   // leaves the request or does not lead back ends the walk (the request is malformed).
   template <class Fn>
   __device__ __forceinline__ void walk(int i, int r0, const int32_t* __restrict__ parent,
                                        const int32_t* __restrict__ draft_tok, Fn&& f) const {
-    if (req[i] < 0) return;
-    const int base = seg_lo, first = lo[i];
+    if (at[i].x < 0) return;
+    const int base = seg_lo, first = at[i].y;
     for (int c = r0 + i; c > first;) {
       const bool in = (unsigned)(c - base) < (unsigned)kPathStage;
       const int d = in ? tok[c - base] : draft_tok[c], p = in ? par[c - base] : parent[c];
@@ -179,154 +182,262 @@ typedef int i32x4 __attribute__((__vector_size__(16)));
 typedef float fx4 __attribute__((__vector_size__(16)));
 
 // The rules on one tile of the LM-head kernel. Its accumulators are only read: the drafted logits' gather
-// (`one`) and the record of a row block (`block`) take each logit through the rules on its way, since a
-// loop whose accumulators are changed behind it has them moved between register files on every pass.
+// takes each of its logits through `one`, and the records come from row blocks that are staged in LDS,
+// kStep at a time, and taken through `block` in a loop of one body. (Changed in place, the accumulators were moved
+// between the register files on every pass of the K loop; with every block's code laid out like the
+// records without rules, it was longer than the instruction cache and took longer to fetch than to
+// run: 378 rows at V = 151936 428 us without rules, 583 with them.)
+//
 // Every tile reads its ids' slice of the table, the bias and the mask once per 16 rows, through the caches:
 // with one request 9 bytes an id beside the weight's H or 2 H.
 //
-// LDS: how often each row's path drafted each of the tile's ids, filled only where `hit` (16 bits hold
-// any path of kMaxRuledRows rows); over it, before it is filled, the gather's list and scratch; behind
-// it the record exchange, the counters and the rows.
+// LDS: the staged blocks, before them the gather's list and scratch; how often each row of a block (of
+// each wave row) drafted each of the tile's ids on its path, in 16 bits, which hold any path of
+// kMaxRuledRows rows, filled for the blocks that have one; the record exchange and the counters; the rows.
 constexpr int kMaxRuledRows = 65535;
 
 template <class F>
 struct TileRules {
   using C = typename F::C;
   using Rows = RuleRows<F::TR>;
-  static constexpr int kPath = F::TR * F::TV * 2;
-  static constexpr int kRedOff = (kPath > C::kRedOff ? kPath : C::kRedOff);
+  static constexpr int kPitch = F::TV + 8;    // rows 4 banks apart
+  static constexpr int kPath = F::WR * 16 * kPitch * 2;
+  // as many blocks as a CU's LDS holds, or, where the ring leaves room for two workgroups, as half of it
+  static constexpr int kList = F::TR == 256 ? 256 : 4 * F::TR;
+  struct PathList {
+    int n, steps;              // entries (kList kept), bit j: a row of block j has one
+    int at[kList];             // row << 16 | id, from r0 and v0
+  };
+  static constexpr int kFixed =
+      kPath + (C::kCntOff - C::kRedOff) + 32 + (int)(sizeof(Rows) + sizeof(PathList));
+  static constexpr int kRoom = (C::kLds <= 80 * 1024 ? 80 : 160) * 1024 - kFixed;
+  static constexpr int kBlockBytes = C::kWaves * C::MV * 1024;
+  static constexpr int steps() {
+    int n = C::MR;
+    while (n * kBlockBytes > kRoom || C::MR % n != 0) --n;
+    return n;
+  }
+  static constexpr int kStep = steps();
+  static constexpr int kStage = kStep * kBlockBytes > C::kRedOff ? kStep * kBlockBytes : C::kRedOff;
+  static constexpr int kRedOff = kStage + kPath;
   static constexpr int kCntOff = kRedOff + (C::kCntOff - C::kRedOff);
   static constexpr int kRowsOff = (kCntOff + 8 + 15) / 16 * 16;
-  static constexpr int kBytes = kRowsOff + (int)sizeof(Rows);
+  static constexpr int kBytes = kRowsOff + (int)(sizeof(Rows) + sizeof(PathList));
   static_assert(F::MF::kBlock == 16 && F::MF::kRegs == 4, "four consecutive ids a lane and block");
   const RuleArgs& r;
   const int32_t* parent;
   const int32_t* draft_tok;
   int N, V, v0, v_end, r0, lane, wr, vw;
-  uint16_t* path;
+  char* lds;
   Rows& rows;
-  bool hit, wide_c, wide_b;
-  float unit;
+  bool wide_c, wide_b;
+  uint32_t paths;              // bit j: a row of block j has one of the tile's ids on its path
 
   template <class A, class P>
   __device__ __forceinline__ TileRules(const RuleArgs& r_, const A& a, int v0_, int v_end_, int r0_,
                                        void* smem, const P& pre)
       : r(r_), parent(a.parent), draft_tok(a.draft_tok), N(a.N), V(a.V), v0(v0_), v_end(v_end_),
-        r0(r0_), path(static_cast<uint16_t*>(smem)),
-        rows(*reinterpret_cast<Rows*>(static_cast<char*>(smem) + kRowsOff)) {
+        r0(r0_), lds(static_cast<char*>(smem)), rows(*reinterpret_cast<Rows*>(static_cast<char*>(smem) + kRowsOff)) {
     rows.template build<C::kThreads>(r, a.req_offsets, parent, draft_tok, a.B, N, r0, v0, v_end, pre);
-    hit = __builtin_amdgcn_readfirstlane(rows.hit);
-    unit = opaque_one();
     lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     wr = wave / F::WV;
     vw = (wave % F::WV) * C::kWaveV + 4 * (lane >> 4);    // this lane's ids of block 0, from v0
-    wide_c = (V & 3) == 0 && (reinterpret_cast<uintptr_t>(r.counts) & 15) == 0;
-    wide_b = (r.bias_pitch & 3) == 0 && (V & 3) == 0 &&
-             (reinterpret_cast<uintptr_t>(r.bias) & 15) == 0;
+    wide_c = V % 4 == 0 && reinterpret_cast<uintptr_t>(r.counts) % 16 == 0;
+    wide_b = V % 4 == 0 && r.bias_pitch % 4 == 0 && reinterpret_cast<uintptr_t>(r.bias) % 16 == 0;
+  }
+
+  __device__ __forceinline__ PathList& list() const {
+    return *reinterpret_cast<PathList*>(lds + kRowsOff + sizeof(Rows));
   }
 
   // The logit z of id v0 + dv in row r0 + i, for one lane.
   __device__ __forceinline__ float one(int i, int dv, float z) const {
-    const int b = rows.req[i], v = v0 + dv;
+    const int b = rows.req(i), v = v0 + dv;
     if (b < 0) return z;
     int n = 0;
     rows.walk(i, r0, parent, draft_tok, [&](int d) { n += d == v; });
-    z = penalised(z, r.counts ? r.counts[(size_t)b * V + v] : 0, n, rows.rule[i]);
+    z = penalised(z, r.counts ? r.counts[(size_t)b * V + v] : 0, n, rows.rule(i, r0));
     if (r.bias) z = __fadd_rn(z, r.bias[(size_t)b * r.bias_pitch + v]);
     if (r.allowed && !((r.allowed[(size_t)(r0 + i) * r.words + (v >> 5)] >> (v & 31)) & 1))
       z = kNegInf;
     return z;
   }
 
-  // Between the gather and the first block, by every thread.
-  __device__ __forceinline__ void fill_paths() {
-    if (!hit) return;
-    constexpr int T = C::kThreads;
-    uint32_t* words = reinterpret_cast<uint32_t*>(path);
-    for (int i = threadIdx.x; i < kPath / 4; i += T) words[i] = 0;
+  // Between the gather and the first block, by every thread: every row's path once, all rows side by side,
+  // its ids of this tile into a list. (A walk is a chain of LDS reads, 0.15 us a node: walked again for
+  // every block, a path of 24 nodes cost a tile that had one of its ids 20 us.)
+  __device__ __forceinline__ void find_paths() {
+    PathList& l = list();
     __syncthreads();
-    for (int i = threadIdx.x; i < min(F::TR, N - r0); i += T)
-      rows.walk(i, r0, parent, draft_tok, [&](int d) {
-        if (d >= v0 && d < v_end) ++path[i * F::TV + d - v0];
-      });
+    if (threadIdx.x == 0) l.n = l.steps = 0;
     __syncthreads();
+    if (rows.hit)
+      for (int i = threadIdx.x; i < min(F::TR, N - r0); i += C::kThreads) {
+        bool any = false;
+        rows.walk(i, r0, parent, draft_tok, [&](int d) {
+          if (d < v0 || d >= v_end) return;
+          any = true;
+          const int k = atomicAdd(&l.n, 1);
+          if (k < kList) l.at[k] = i << 16 | (d - v0);
+        });
+        if (any) atomicOr(&l.steps, 1 << (i % C::kWaveR / 16));
+      }
+    __syncthreads();
+    paths = __builtin_amdgcn_readfirstlane(l.steps);
+  }
+  __device__ __forceinline__ uint16_t* path() const {
+    return reinterpret_cast<uint16_t*>(lds + kStage);
+  }
+  // The paths of block j, by every thread: from the list, or, where it was too short, by walking them.
+  __device__ __forceinline__ void fill_paths(int j) const {
+    uint32_t* words = reinterpret_cast<uint32_t*>(path());
+    const PathList& l = list();
+    __syncthreads();
+    for (int i = threadIdx.x; i < kPath / 4; i += C::kThreads) words[i] = 0;
+    __syncthreads();
+    if (l.n <= kList) {
+      for (int k = threadIdx.x; k < l.n; k += C::kThreads) {
+        const int i = l.at[k] >> 16, id = l.at[k] & 0xffff;
+        if (i % C::kWaveR / 16 != j) continue;
+        const int at = (i / C::kWaveR * 16 + i % 16) * kPitch + id;
+        atomicAdd(&words[at >> 1], 1u << (16 * (at & 1)));
+      }
+    } else {
+      const int t = threadIdx.x, i = t / 16 * C::kWaveR + 16 * j + t % 16;
+      if (t < 16 * F::WR && i < N - r0)
+        rows.walk(i, r0, parent, draft_tok, [&](int d) {
+          if (d >= v0 && d < v_end) ++path()[t * kPitch + d - v0];
+        });
+    }
+    __syncthreads();
+  }
+
+  // Row block j of this wave, in the staged blocks: 16 bytes of lane l and 16-id block i at [i][l].
+  __device__ __forceinline__ fx4* staged(int j) const {
+    return reinterpret_cast<fx4*>(lds) +
+           ((threadIdx.x >> 6) * kStep + j % kStep) * (C::MV * kWave);
   }
 
   // What a lane holds of the table and the bias for its ids, for the request of its last row, and of the
   // mask for its next row: the rows of a block mostly belong to one request, the block before's, and
-  // the mask's words are on their way while a block is computed.
+  // the mask's words are on their way while a block is computed. Every load is from a place inside its
+  // array, whatever the row and the ids; what it brings of other rows and ids is masked or discarded.
   struct Held {
-    int b = -1;
+    int b = -2;
+    bool fresh = false;            // c is new
+    uint32_t seen = 0;             // bit i: some lane's entries of 16-id block i are in the table
+    uint32_t ids = 0;              // bit 4 i + e: entry e of block i is one of the tile's ids
     i32x4 c[C::MV];
     fx4 bias[C::MV];
     uint32_t bits[C::MV];
   };
+  static_assert(4 * C::MV <= 32, "a bit per entry");
+  template <class T4, class T>
+  __device__ __forceinline__ void load_ids(const T* __restrict__ row, bool wide,
+                                           T4 (&x)[C::MV]) const {
+    if (wide) {
+      static_for<C::MV>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        x[i] = *reinterpret_cast<const T4*>(row + min(v0 + vw + 16 * i, V - 4));
+      });
+    } else {
+      static_for<4 * C::MV>([&](auto ec) {
+        constexpr int i = decltype(ec)::value / 4, e = decltype(ec)::value % 4;
+        x[i][e] = row[min(v0 + vw + 16 * i + e, V - 1)];
+      });
+    }
+  }
   __device__ __forceinline__ void load_bits(int j, uint32_t (&bits)[C::MV]) const {
-    const int i_row = wr * C::kWaveR + 16 * j + (lane & 15);
-    const bool on = rows.req[i_row] >= 0;
+    if (!r.allowed) return;
+    const int n = min(r0 + wr * C::kWaveR + 16 * j + (lane & 15), N - 1);
+    const uint32_t* row = r.allowed + (size_t)n * r.words;
     static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
-      const int v = v0 + vw + 16 * i;
-      bits[i] = ~0u;
-      if (r.allowed && on && v < v_end)
-        bits[i] = r.allowed[(size_t)(r0 + i_row) * r.words + (v >> 5)] >> (v & 31);
+      bits[i] = row[min((v0 + vw + 16 * i) >> 5, r.words - 1)];
     });
   }
+  __device__ __forceinline__ void load_request(int b, Held& h) const {
+    if (r.counts) load_ids(r.counts + (size_t)b * V, wide_c, h.c);
+    if (r.bias) load_ids(r.bias + (size_t)b * r.bias_pitch, wide_b, h.bias);
+    h.b = b;
+    h.fresh = true;
+  }
+  // Ahead of the gather, which covers the loads.
   __device__ __forceinline__ void begin(Held& h) const {
     static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
       h.c[i] = i32x4{};
       h.bias[i] = fx4{};
+      h.bits[i] = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        h.ids |= (uint32_t)(v0 + vw + 16 * i + e < v_end) << (4 * i + e);
     });
     load_bits(0, h.bits);
+    load_request(max(rows.req(wr * C::kWaveR + (lane & 15)), 0), h);
   }
 
-  // z[4 i + e]: the ruled logits of row block j, acc[i][e]; blocks in order, begin() before the first.
-  __device__ __forceinline__ void block(int j, const typename F::MF::Acc (&acc)[C::MV],
-                                        float (&z)[4 * C::MV], Held& h) const {
+  // Row block j through the rules, into z[4 i + e], -inf past the tile's ids; blocks in order, begin()
+  // before the first. Rows of no request give no results (their offsets are malformed).
+  __device__ __forceinline__ void block(int j, float (&z)[4 * C::MV], Held& h) const {
     const int i_row = wr * C::kWaveR + 16 * j + (lane & 15);
-    const int b = rows.req[i_row];
-    const bool on = b >= 0;
-    if (!__all(b == h.b)) {
+    const int b = max(rows.req(i_row), 0);
+    if (!__all(b == h.b)) load_request(b, h);
+    if (h.fresh && r.counts) {
+      h.seen = 0;
       static_for<C::MV>([&](auto ic) {
         constexpr int i = decltype(ic)::value;
-        const int v = v0 + vw + 16 * i;
-        h.c[i] = i32x4{};
-        h.bias[i] = fx4{};
-        if (on && v < v_end) {
-          if (r.counts) h.c[i] = load4<i32x4>(r.counts + (size_t)b * V, v, V, wide_c);
-          if (r.bias) h.bias[i] = load4<fx4>(r.bias + (size_t)b * r.bias_pitch, v, V, wide_b);
-        }
+        if (__any((h.c[i][0] | h.c[i][1] | h.c[i][2] | h.c[i][3]) != 0)) h.seen |= 1u << i;
       });
-      h.b = b;
     }
-    const RowRule rr = rows.rule[i_row];
-    uint32_t bits[C::MV];
-    static_for<C::MV>([&](auto ic) { bits[decltype(ic)::value] = h.bits[decltype(ic)::value]; });
+    h.fresh = false;
+    uint32_t keep = h.ids;
+    if (r.allowed) {
+      uint32_t on = 0;
+      static_for<C::MV>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        on |= ((h.bits[i] >> ((v0 + vw + 16 * i) & 31)) & 15u) << (4 * i);
+      });
+      keep &= on;
+    }
     if (j + 1 < C::MR) load_bits(j + 1, h.bits);
+    const fx4* from = staged(j);
     static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
-      const uint2 p4 = hit && on
-                           ? *reinterpret_cast<const uint2*>(&path[i_row * F::TV + vw + 16 * i])
-                           : make_uint2(0u, 0u);
-      const i32x4 c = h.c[i];
-      const bool special = !__all((c[0] | c[1] | c[2] | c[3] | (int)(p4.x | p4.y)) == 0);
-      float y[4];
+      const fx4 y = from[i * kWave + lane];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = __fmul_rn(acc[i][e], unit);
-      if (special) {
+      for (int e = 0; e < 4; ++e) z[4 * i + e] = y[e];
+    });
+    const bool with_path = (paths >> j) & 1;
+    const uint32_t seen = with_path ? ~0u : h.seen;
+    if (seen != 0) {
+      const RowRule rr = rows.rule(i_row, r0);
+      const uint16_t* my_path = path() + (wr * 16 + (lane & 15)) * kPitch + vw;
+      static_for<C::MV>([&](auto ic) {
+        constexpr int i = decltype(ic)::value;
+        if ((seen >> i) & 1) {
+          const uint2 p4 = with_path ? *reinterpret_cast<const uint2*>(my_path + 16 * i)
+                                     : make_uint2(0u, 0u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int n_path = ((e < 2 ? p4.x : p4.y) >> (16 * (e & 1))) & 0xffff;
-          y[e] = penalised(y[e], c[e], n_path, rr);
+          for (int e = 0; e < 4; ++e) {
+            const int n_path = ((e < 2 ? p4.x : p4.y) >> (16 * (e & 1))) & 0xffff;
+            z[4 * i + e] = penalised(z[4 * i + e], h.c[i][e], n_path, rr);
+          }
         }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (r.bias) y[e] = __fadd_rn(y[e], h.bias[i][e]);
-        z[4 * i + e] = (bits[i] >> e) & 1 ? y[e] : kNegInf;
-      }
+      });
+    }
+    if (r.bias) {
+      static_for<4 * C::MV>([&](auto ec) {
+        constexpr int i = decltype(ec)::value / 4, e = decltype(ec)::value % 4;
+        z[4 * i + e] = __fadd_rn(z[4 * i + e], h.bias[i][e]);
+      });
+    }
+    // a bit of `keep` as a mask over the value: set, the value, else -inf
+    static_for<4 * C::MV>([&](auto kc) {
+      constexpr int k = decltype(kc)::value;
+      const uint32_t m = (uint32_t)__builtin_amdgcn_sbfe((int)keep, k, 1);
+      z[k] = __uint_as_float((__float_as_uint(z[k]) & m) | (0xff800000u & ~m));
     });
   }
 };
@@ -385,7 +496,7 @@ void k_adjust(AdjustArgs a) {
   int c[PT];
   float bias[PT];
   for (int n = r0; n < r_end; ++n) {
-    const int i = n - r0, b = rows.req[i];
+    const int i = n - r0, b = rows.req(i);
     float z[PT];
     if (wide_in) {
       const Tv x = *reinterpret_cast<const Tv*>(in + (size_t)n * a.in_pitch + v);
@@ -414,7 +525,7 @@ void k_adjust(AdjustArgs a) {
           }
         }
       }
-      const RowRule rr = rows.rule[i];
+      const RowRule rr = rows.rule(i, r0);
       int path[PT] = {};
       if (hit)
         rows.walk(i, r0, a.parent, a.draft_tok, [&](int d) {
