@@ -371,11 +371,12 @@ struct Layout {
   size_t bytes = 0;
 };
 
-Layout layout(int B, int N, int V) {
+// records: of the LM head over all rows (0: K1's most).
+Layout layout(int B, int N, int V, size_t records = 0) {
   Layout L;
   L.S = (V + kSlab - 1) / kSlab;
   L.n_conf = (V + kConfChunk - 1) / kConfChunk;
-  const size_t rec = max_records(N, V) * 4;
+  const size_t rec = std::max(records, max_records(N, V)) * 4;
   const size_t conf = (size_t)B * L.n_conf * 4;
   size_t at = 0;
   L.off_rec_m = at;  at += align_up(rec);

@@ -68,50 +68,145 @@ int round_rows(const uint16_t* hidden, const void* w, int N, int H, int V, char*
 
 // ---- launches of the 8-bit LM head
 
-using Q8Rows64 = Q8Family<256, 64, 4, 1, 3, 0, true>;
-using Q8Rows128 = Q8Family<256, 128, 2, 2, 3, 3, true>;
-using Q8Rows192 = Q8Family<256, 192, 2, 2, 3, 3, false>;
-using Q8Rows256 = Q8Family<256, 256, 2, 2, 3, 3, false>;
+// Up to 64 rows: the tiles of 64, 128 and 256 ids by what share of the ids a CU has.
+using Q8Ids64 = Q8Family<64, 64, 4, false>;
+using Q8Ids128 = Q8Family<128, 64, 3, false>;
+using Q8Ids256 = Q8Family<256, 64, 2, false>;
+// Beyond: tiles of 256 ids, and what the tail of a launch runs.
+template <int TR> using Q8Rows = Q8Family<256, TR, 3, true>;
+template <int TR, int IDS> using Q8Tail = Q8Family<IDS, TR, TR == 256 ? 2 : 3, false>;
 
-// f(family tag, launch) for the launches of N rows: K1's plan over whole slabs.
+constexpr int kQ8Group = 16;          // slab widths: 16 ids share a scale
+constexpr int kQ8MinCut = 48;         // narrowest slab up to 64 rows
+
+// ids of a slab when n slabs share `ids`
+int q8_share(int64_t ids, int64_t n) {
+  return (int)std::max<int64_t>(kQ8MinCut,
+                                ((ids + n - 1) / n + kQ8Group - 1) / kQ8Group * kQ8Group);
+}
+
+// Most records that a step of up to N rows writes, whatever the CU count (see max_records).
+size_t q8_max_records(int N, int V) {
+  const size_t narrow = (V + kQ8MinCut - 1) / kQ8MinCut, whole = (V + kSlab - 1) / kSlab;
+  size_t n = std::min(N, 64) * narrow;
+  if (N > 64) n = std::max(n, N * (whole + std::min<size_t>(narrow, kMaxCutTail)));
+  return n;
+}
+
+struct Q8Plan {
+  int rows;          // tile rows: 64, 128, 192 or 256
+  int ids;           // 64 rows: ids of the tile; else ids of the tail's tile
+  SlabCut cut;
+  int S;             // slabs in all
+  int64_t est;       // beyond 64 rows
+};
+
+// Up to 64 rows, in us at 60 rows and H = 4096 on weights that are not in the caches (a read at 7 TB/s, the
+// rule's choice, the best of 24 others): V = 8000 5, 25, 25; 16000 9, 25, 25; 24000 14, 31, 31; 32000
+// 19, 34, 31; 40000 23, 39, 39; 50000 29, 43, 43; 64000 37, 48, 47; 80000 47, 65, 63; 100000 59, 69, 69;
+// 128256 75, 81, 81; 140000 82, 106, 106; 151936 89, 113, 113; 200000 117, 140, 138; 260000 152, 159, 159.
+Q8Plan q8_rows64(int V, int cus) {
+  auto even = [&](int ids, int width) {
+    const int S = (V + width - 1) / width;
+    return Q8Plan{64, ids, SlabCut{S, width, width, 0, 0}, S, 0};
+  };
+  const int64_t c = cus;
+  const int two = q8_share(V, 2 * c);
+  if (V <= c * 64) return even(64, 64);
+  if (two <= 64) return even(64, two);
+  if (two <= 128) return even(128, two);
+  if (two <= 256) return even(256, two);
+  if (V <= 3 * c * 256) return even(128, 128);
+  // whole pairs of shares, which a CU runs side by side
+  return even(256, q8_share(V, 2 * c * ((V + 512 * c - 1) / (512 * c))));
+}
+
+// Beyond: whole rounds of 256-id tiles and a tail of one narrower tile a CU, where that is estimated to
+// be faster than the best plan over whole slabs. Costs as K1's (its rounds are in the same proportion here:
+// 64, 77 and 97 us); a round of tails of 64 and 128 ids as K1's.
+Q8Plan q8_tail_plan(int N, int V, int cus, int64_t plan_est) {
+  struct Family { int rows, cost, tail64, tail128; };
+  const Family families[3] = {{128, 62, 30, 44}, {192, 80, 36, 54}, {256, 98, 44, INT32_MAX}};
+  Q8Plan best{};
+  best.est = plan_est;
+  for (const Family& f : families) {
+    const int RT = (N + f.rows - 1) / f.rows, per_round = cus / RT;
+    if (per_round < 1) continue;
+    const int64_t rounds = V / ((int64_t)kSlab * per_round);
+    const int n_main = (int)(rounds * per_round), rest = V - n_main * kSlab;
+    const int width = q8_share(rest, per_round), n_tail = (rest + width - 1) / width;
+    if (rest == 0 || width > 128 || n_tail > kMaxCutTail) continue;
+    const int ids = width <= 64 ? 64 : 128;
+    const int64_t tail = ids == 64 ? f.tail64 : f.tail128, est = rounds * f.cost + tail;
+    if (tail == INT32_MAX || est >= best.est) continue;
+    best = Q8Plan{f.rows, ids, SlabCut{n_main, kSlab, width, 0, 0},
+                  n_main + n_tail, est};
+  }
+  return best;
+}
+
+// f(main family, tail family, cut, tiles of the tail, launch) for the launches of N rows; returns the
+// records a row writes.
 template <class Fn>
-void q8_launches(int N, int V, int cus, Fn&& f) {
-  const int S = (V + kSlab - 1) / kSlab;
-  asv_k1_launch k[2];
-  const int n = k1_launches(N, S, cus, plan_k1(N, S, cus), k);
-  for (int q = 0; q < n; ++q) switch (k[q].tile_rows) {
-      case 64: f(Q8Rows64{}, k[q]); break;
-      case 128: f(Q8Rows128{}, k[q]); break;
-      case 192: f(Q8Rows192{}, k[q]); break;
-      default: f(Q8Rows256{}, k[q]); break;
+int q8_launches(int N, int V, int cus, Fn&& f) {
+  asv_k1_launch k{};
+  if (N <= 64) {
+    const Q8Plan p = q8_rows64(V, cus);
+    k.row_tiles = 1;
+    switch (p.ids) {
+      case 64: f(Q8Ids64{}, Q8Ids64{}, p.cut, 0, k); break;
+      case 128: f(Q8Ids128{}, Q8Ids128{}, p.cut, 0, k); break;
+      default: f(Q8Ids256{}, Q8Ids256{}, p.cut, 0, k); break;
     }
+    return p.S;
+  }
+  const int S = (V + kSlab - 1) / kSlab;
+  int64_t est = 0;
+  const K1Plan plan = plan_k1(N, S, cus, &est);
+  const Q8Plan p = q8_tail_plan(N, V, cus, est);
+  if (p.rows) {
+    k.row_tiles = (N + p.rows - 1) / p.rows;
+    tile_blocking(k.row_tiles, cus, &k.blk_slabs, &k.blk_rows);
+    const int tail = (p.S - p.cut.n_main) * k.row_tiles;
+    if (p.rows == 128 && p.ids == 64) f(Q8Rows<128>{}, Q8Tail<128, 64>{}, p.cut, tail, k);
+    else if (p.rows == 128) f(Q8Rows<128>{}, Q8Tail<128, 128>{}, p.cut, tail, k);
+    else if (p.rows == 192 && p.ids == 64) f(Q8Rows<192>{}, Q8Tail<192, 64>{}, p.cut, tail, k);
+    else if (p.rows == 192) f(Q8Rows<192>{}, Q8Tail<192, 128>{}, p.cut, tail, k);
+    else f(Q8Rows<256>{}, Q8Tail<256, 64>{}, p.cut, tail, k);
+    return p.S;
+  }
+  asv_k1_launch launches[2];
+  const int n = k1_launches(N, S, cus, plan, launches);
+  for (int q = 0; q < n; ++q) {
+    const asv_k1_launch& l = launches[q];
+    const SlabCut cut{l.n_slabs, kSlab, kSlab, l.slab0, l.slab0 * kSlab};
+    switch (l.tile_rows) {
+      case 128: f(Q8Rows<128>{}, Q8Tail<128, 64>{}, cut, 0, l); break;
+      case 192: f(Q8Rows<192>{}, Q8Tail<192, 64>{}, cut, 0, l); break;
+      default: f(Q8Rows<256>{}, Q8Tail<256, 64>{}, cut, 0, l); break;
+    }
+  }
+  return S;
 }
 
-SlabCut whole_slabs(const asv_k1_launch& k) {
-  return SlabCut{k.n_slabs, kSlab, kSlab, k.slab0, k.slab0 * kSlab};
-}
-
-template <class T>
-void launch_logits(const LmheadArgs& g, const asv_logits_args* a, hipStream_t s) {
-  q8_launches(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
-    using F = decltype(family);
-    k_lmhead_logits<F, T><<<k.n_slabs * k.row_tiles, F::C::kThreads, 0, s>>>(
-        g, whole_slabs(k), k.row_tiles, k.blk_slabs, k.blk_rows, static_cast<T*>(a->out),
-        a->out_pitch);
-  });
+// What the launches of N rows will write a row.
+int q8_records(int N, int V, int cus) {
+  return q8_launches(N, V, cus, [](auto, auto, const SlabCut&, int, const asv_k1_launch&) {});
 }
 
 template <class E>
 int verify_fp8(const asv_verify_args* a, char* ws, hipStream_t s, const E& e) {
-  const Layout L = layout(a->B, a->N, a->V);
+  const Layout L = layout(a->B, a->N, a->V, q8_max_records(a->N, a->V));
+  const int cus = cu_count(), S = q8_records(a->N, a->V, cus);
   (void)hipGetLastError();
-  const int S = (a->V + kSlab - 1) / kSlab;
   LmheadArgs g = lmhead_args(a, L, ws, S);
   if (int rc = round_rows(a->hidden, a->w_lm, a->N, a->H, a->V, ws + L.bytes, s, &g)) return rc;
   if (int rc = draft_conf(a, L, ws, a->N <= 64 ? S : 0, s, &g.conf)) return rc;
-  q8_launches(a->N, a->V, cu_count(), [&](auto family, const asv_k1_launch& k) {
-    launch_lmhead<decltype(family)>(g, whole_slabs(k), 0, k, s, K1Events{nullptr, nullptr}, e);
-  });
+  q8_launches(a->N, a->V, cus,
+              [&](auto m, auto t, const SlabCut& cut, int n_tail, const asv_k1_launch& k) {
+                launch_lmhead<decltype(m), decltype(t)>(g, cut, n_tail, k, s,
+                                                        K1Events{nullptr, nullptr}, e);
+              });
   if (int rc = launch_status("k_lmhead_partial")) return rc;
   return finish_verify<E::kRules>(a, L, ws, S, s);
 }
@@ -188,11 +283,14 @@ extern "C" int asv_lm_head_logits(const asv_logits_args* a, void* workspace,
   g.V = a->V;
   if (int rc = round_rows(a->hidden, a->w, a->N, a->H, a->V, static_cast<char*>(workspace), s, &g))
     return rc;
-  switch (a->out_type) {
-    case ASV_F32: launch_logits<float>(g, a, s); break;
-    case ASV_BF16: launch_logits<__bf16>(g, a, s); break;
-    default: launch_logits<_Float16>(g, a, s); break;
-  }
+  const StoreArgs st{a->out, a->out_pitch, a->out_type};
+  q8_launches(a->N, a->V, cu_count(),
+              [&](auto m, auto t, const SlabCut& cut, int n_tail, const asv_k1_launch& k) {
+                using M = decltype(m);
+                k_lmhead_logits<M, decltype(t)>
+                    <<<cut.n_main * k.row_tiles + n_tail, M::C::kThreads, 0, s>>>(
+                        g, cut, k.row_tiles, k.blk_slabs, k.blk_rows, st);
+              });
   return launch_status("k_lmhead_logits");
 }
 
@@ -204,7 +302,7 @@ extern "C" int asv_verify_ruled_workspace_bytes(int32_t B, int32_t N, int32_t H,
   }
   uint64_t codes = 0, total = 0;
   if (!bytes || !sizes_ok(B, N, H, V) || !fp8_size(V, H, &codes, &total)) return ASV_EINVAL;
-  *bytes = layout(B, N, V).bytes + rounded_bytes(N, H);
+  *bytes = layout(B, N, V, q8_max_records(N, V)).bytes + rounded_bytes(N, H);
   return ASV_OK;
 }
 

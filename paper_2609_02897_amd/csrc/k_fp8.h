@@ -175,21 +175,22 @@ struct Q8Cfg {
                        kWaveR = B::kWaveR, MV = B::MV, MR = B::MR, NS = B::NS, kCand = B::kCand,
                        kCap = B::kCap, kScrOff = B::kScrOff, kRedOff = B::kRedOff,
                        kCntOff = B::kCntOff;
-  static constexpr int kStageW = TV * 64, kStageX = TR * 128, kStage = kStageW + kStageX;
+  static constexpr int kStageW = TV * 64, kStageX = TR * 128, kOffX = NST * kStageW;
   static constexpr int DW = kStageW / 1024 / kWaves, DX = kStageX / 1024 / kWaves;
   static constexpr int kLoads = DW + DX;
-  static constexpr int kLds = NST * kStage;
+  static constexpr int kLds = NST * (kStageW + kStageX);
   static_assert(DW >= 1 && DX >= 1 && DW * kWaves * 1024 == kStageW &&
                 DX * kWaves * 1024 == kStageX, "each wave copies whole 1 KB groups");
-  static_assert(NST >= 2 && NST <= 5 && (NST - 2) * kLoads <= 63, "ring depth, vmcnt range");
+  static_assert(NST >= 2 && NST <= 5, "ring depth");
   static_assert(kCntOff + 8 <= kLds && kLds <= 160 * 1024, "LDS per workgroup");
 };
 
-// A tile family of the 8-bit LM head (see TileFamily). LOOP: 0 the burst ring, 3 the spread loop.
-template <int TV_, int TR_, int WV_, int WR_, int NST_, int LOOP_, bool STREAM_W_>
+// A tile family of the 8-bit LM head (see TileFamily), its waves along the ids. SPREAD: the spread K loop,
+// else the burst ring, which copies W with the non-temporal hint.
+template <int TV_, int TR_, int NST_, bool SPREAD_>
 struct Q8Family {
-  static constexpr int TV = TV_, TR = TR_, WV = WV_, WR = WR_, BK = 64, NST = NST_, LOOP = LOOP_;
-  static constexpr bool STREAM_W = STREAM_W_, kFp8 = true;
+  static constexpr int TV = TV_, TR = TR_, WV = 4, WR = 1, BK = 64, NST = NST_;
+  static constexpr bool kFp8 = true, kSpread = SPREAD_;
   using MF = Mfma16;
   using C = Q8Cfg<TV, TR, WV, WR, NST>;
   static __device__ __forceinline__ void logits(const LmheadArgs& a, int v0, int v_end, int r0,
@@ -206,7 +207,7 @@ struct Q8Io {
   int lane, wave, lds0, w_frag0, x_frag0[C::NS];
   unsigned w_kstep;
   __amdgpu_buffer_rsrc_t w_rsrc, x_rsrc;
-  int w_voff[C::DW], x_voff[C::DX];
+  int v_rows, x_pitch;
   ConstWords wa, wb;                  // scales of the wave's first block of 128 ids and of the next
   int split;                          // 16-id blocks i >= split take wb
 
@@ -220,7 +221,7 @@ struct Q8Io {
     w_frag0 = q8_swz(wv * C::kWaveV + row, grp);
     static_for<C::NS>([&](auto sc) {
       constexpr int s = decltype(sc)::value;
-      x_frag0[s] = C::kStageW / 16 + swz<8>(wr * C::kWaveR + row, 4 * s + grp);
+      x_frag0[s] = C::kOffX / 16 + swz<8>(wr * C::kWaveR + row, 4 * s + grp);
     });
     lds0 = __builtin_amdgcn_readfirstlane((int)(size_t)smem);
     const unsigned Vp = ((unsigned)a.V + 255) / 256 * 256;
@@ -234,41 +235,30 @@ struct Q8Io {
     const int r_last = min(r0 + F::TR, a.N) - 1;
     x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.X + (size_t)r0 * a.H),
                                                (short)0, (r_last + 1 - r0) * a.H * 2, kRsrcWord3);
-    static_for<C::DW>([&](auto ic) {   // copy j: ids 16 j .. 16 j + 15, four lanes an id
-      constexpr int i = decltype(ic)::value;
-      const int r = (i * C::kWaves + wave) * 16 + lane / 4;
-      w_voff[i] = r < w_rows ? r * 64 + (q8_swz(r, lane & 3) & 3) * 16 : (int)0x80000000;
-    });
-    static_for<C::DX>([&](auto ic) {   // copy j: rows 8 j .. 8 j + 7, eight lanes a row
-      constexpr int i = decltype(ic)::value;
-      const int r = (i * C::kWaves + wave) * 8 + lane / 8;
-      x_voff[i] = r * a.H * 2 + ((lane & 7) ^ swz_phase<8>(r)) * 16;
-    });
+    v_rows = w_rows;
+    x_pitch = a.H * 2;
     const int vw = v0 + wv * C::kWaveV, blk = vw / kQBlock, last = (int)(Vp / kQBlock) - 1;
     const uintptr_t base = reinterpret_cast<uintptr_t>(a.w_scale);
     wa = (ConstWords)(base + (size_t)min(blk, last) * a.scale_pitch);
     wb = (ConstWords)(base + (size_t)min(blk + 1, last) * a.scale_pitch);
     split = ((blk + 1) * kQBlock - vw) / 16;
   }
-  // copy c of this wave (W first) of K stage ks into ring slot `slot`
-  template <int c>
-  __device__ __forceinline__ void copy(int slot, int ks) const {
-    const int base = lds0 + slot * C::kStage;
-    if constexpr (c < C::DW) {
-      const int at = base + (c * C::kWaves + wave) * 1024;
-      const int so = __builtin_amdgcn_readfirstlane((int)((unsigned)ks * w_kstep));
-      if constexpr (F::STREAM_W) dma16_stream(at, w_voff[c], so, w_rsrc);
-      else dma16(at, w_voff[c], so, w_rsrc);
-    } else
-      dma16(base + C::kStageW + ((c - C::DW) * C::kWaves + wave) * 1024, x_voff[c - C::DW],
-            __builtin_amdgcn_readfirstlane(ks * 128), x_rsrc);
+  // byte offsets at K stage 0 of this lane's 16 bytes of copy j of a stage: ids 16 j .. 16 j + 15 of W,
+  // four lanes an id; rows 8 j .. 8 j + 7 of X, eight lanes a row
+  __device__ __forceinline__ int w_voff(int j) const {
+    const int r = j * 16 + lane / 4;
+    return r < v_rows ? r * 64 + (q8_swz(r, lane & 3) & 3) * 16 : (int)0x80000000;
+  }
+  __device__ __forceinline__ int x_voff(int j) const {
+    const int r = j * 8 + lane / 8;
+    return r * x_pitch + ((lane & 7) ^ swz_phase<8>(r)) * 16;
   }
   // the codes of 16-id block i for both matrix steps of a stage; the fragment of X block j for step s
   __device__ __forceinline__ uint4 w_codes(int slot, int i) const {
-    return (lds + slot * (C::kStage / 16) + w_frag0)[64 * i];
+    return (lds + slot * (C::kStageW / 16) + w_frag0)[64 * i];
   }
   __device__ __forceinline__ bf16x8 x_frag(int slot, int s, int j) const {
-    return __builtin_bit_cast(bf16x8, (lds + slot * (C::kStage / 16) + x_frag0[s])[128 * j]);
+    return __builtin_bit_cast(bf16x8, (lds + slot * (C::kStageX / 16) + x_frag0[s])[128 * j]);
   }
   // the scales of K stage ks, of the wave's first block of ids and of the next one: the words that hold
   // them, and the scales themselves
@@ -309,8 +299,27 @@ __device__ __forceinline__ void q8_ring(const LmheadArgs& a, int v0, int v_end, 
   constexpr int NST = F::NST;
   const Q8Io<F> io(a, v0, v_end, r0, smem);
   const int KT = a.H / F::BK;
+  int w_voff[C::DW], x_voff[C::DX];
+  static_for<C::DW>([&](auto c) {
+    w_voff[decltype(c)::value] = io.w_voff(decltype(c)::value * C::kWaves + io.wave);
+  });
+  static_for<C::DX>([&](auto c) {
+    x_voff[decltype(c)::value] = io.x_voff(decltype(c)::value * C::kWaves + io.wave);
+  });
+  static_assert((NST - 2) * C::kLoads <= 63, "vmcnt range");
   auto issue_stage = [&](int ks) {
-    static_for<C::kLoads>([&](auto cc) { io.template copy<decltype(cc)::value>(ks % NST, ks); });
+    const int w_at = io.lds0 + ks % NST * C::kStageW + io.wave * 1024;
+    const int x_at = io.lds0 + C::kOffX + ks % NST * C::kStageX + io.wave * 1024;
+    const int w_so = __builtin_amdgcn_readfirstlane((int)((unsigned)ks * io.w_kstep));
+    const int x_so = __builtin_amdgcn_readfirstlane(ks * 128);
+    static_for<C::DW>([&](auto cc) {
+      constexpr int c = decltype(cc)::value;
+      dma16_stream(w_at + c * C::kWaves * 1024, w_voff[c], w_so, io.w_rsrc);
+    });
+    static_for<C::DX>([&](auto cc) {
+      constexpr int c = decltype(cc)::value;
+      dma16(x_at + c * C::kWaves * 1024, x_voff[c], x_so, io.x_rsrc);
+    });
   };
   zero_acc(acc);
   const int pro = min(NST, KT);
@@ -357,6 +366,9 @@ __device__ __forceinline__ void q8_widen_half(const uint4& c, float step, uint32
 
 // The spread K loop in a three-slot ring, one barrier per stage (see lmhead_tile_spread3): copies, LDS
 // reads and widening stand between the matrix instructions, one position m = (s MV + i) MR + j each.
+// Waves 0 and 1 copy W, waves 2 and 3 X. The waves split the ids only (WV = 4): each id is widened
+// once, and with one wave a SIMD the instructions of a stage count (128 rows at V = 128256, two by two waves
+// and one by four: 133 and 129 us). Deeper rings of either operand change nothing. Per stage k:
 //   m < MR          the X fragments of step 1 of slot k;
 //   m < Q2          the remaining copies of stage k + 2;
 //   m = Q2 - 1      wait until stage k + 1 has landed (only copies of stage k + 2 may be outstanding) +
@@ -368,38 +380,56 @@ __device__ __forceinline__ void q8_widen_half(const uint4& c, float step, uint32
 // fragments. Past the last stage the copies repeat the last stage into slots no later stage reads,
 // and what is read of the stage after the last is discarded.
 template <class F>
-__device__ __forceinline__ void q8_spread3(const LmheadArgs& a, int v0, int v_end, int r0,
-                                           uint4* smem, f32x4 (&acc)[F::C::MV][F::C::MR]) {
+__device__ __forceinline__ void q8_spread(const LmheadArgs& a, int v0, int v_end, int r0,
+                                          uint4* smem, f32x4 (&acc)[F::C::MV][F::C::MR]) {
   using C = typename F::C;
   constexpr int NST = 3, MV = C::MV, MR = C::MR, NS = C::NS, NF = MV + MR;
-  constexpr int NM = NS * MV * MR, G = C::kLoads, Q2 = NM - NF;
-  static_assert(F::NST == NST && NS == 2 && MV % 2 == 0 && MR >= 2, "schedule");
+  constexpr int NM = NS * MV * MR, Q2 = NM - NF;
+  constexpr int GW = C::kStageW / 2048, GX = C::kStageX / 2048, G = GW > GX ? GW : GX;
+  static_assert(F::NST == NST && NS == 2 && C::kWaves == 4 && MR >= 2, "schedule");
   static_assert(Q2 >= MR + 2 && Q2 >= MV * MR, "reads of a stage end before the next one's");
   static_assert(2 * G <= 63, "vmcnt range");
+  // copy c of the wave sits c NM / G positions after the barrier that opens its window; the first n1 of n
+  // fall in the same stage as that barrier
   constexpr auto rel = [](int c) { return c * NM / G; };
-  constexpr int n1 = [&] {
-    int n = 0;
-    for (int c = 0; c < G; ++c) n += Q2 + rel(c) < NM ? 1 : 0;
-    return n;
-  }();
+  constexpr auto first = [=](int n) {
+    int k = 0;
+    for (int c = 0; c < n; ++c) k += Q2 + rel(c) < NM ? 1 : 0;
+    return k;
+  };
+  constexpr int n1w = first(GW), n1x = first(GX), n1 = first(G);
   const Q8Io<F> io(a, v0, v_end, r0, smem);
   const int KT = a.H / F::BK;
-  auto issue_copy = [&](int j, auto cc) {
-    io.template copy<decltype(cc)::value>(j % NST, min(j, KT - 1));
+  const bool is_w = io.wave < 2;
+  const int sub = io.wave & 1;
+  const __amdgpu_buffer_rsrc_t rsrc = is_w ? io.w_rsrc : io.x_rsrc;
+  const unsigned kstep = is_w ? io.w_kstep : 128u;
+  const int n_copies = is_w ? GW : GX;
+  const int slot_bytes = is_w ? C::kStageW : C::kStageX;
+  const int lds_at = io.lds0 + (is_w ? 0 : C::kOffX) + sub * 1024;
+  int voff[G];
+  static_for<G>([&](auto cc) {
+    constexpr int c = decltype(cc)::value;
+    voff[c] = is_w ? io.w_voff(2 * c + sub) : io.x_voff(2 * c + sub);
+  });
+  // copy c of stage j of this wave's operand into ring slot `to`
+  auto issue = [&](int j, int to, auto cc) {
+    constexpr int c = decltype(cc)::value;
+    if (c < (GW < GX ? GW : GX) || c < n_copies)
+      dma16(lds_at + to * slot_bytes + c * 2048, voff[c],
+            __builtin_amdgcn_readfirstlane((int)((unsigned)min(j, KT - 1) * kstep)), rsrc);
   };
   zero_acc(acc);
   uint4 w[MV];
   bf16x8 x[NS][MR];
   uint32_t f[2][4];
 
-  static_for<G>([&](auto cc) { issue_copy(0, cc); });
-  static_for<G>([&](auto cc) { issue_copy(1, cc); });
-  static_for<G>([&](auto cc) {
-    if constexpr (decltype(cc)::value < n1) issue_copy(2, cc);
-  });
+  for (int j = 0; j < NST - 1; ++j) static_for<G>([&](auto cc) { issue(j, j, cc); });
+  static_for<n1>([&](auto cc) { issue(NST - 1, NST - 1, cc); });
   float sa, sb, na, nb;
   io.steps(0, sa, sb);
-  wait_vm_barrier<G + n1>();
+  if (is_w) wait_vm_barrier<GW + n1w>();
+  else wait_vm_barrier<GX + n1x>();
   static_for<MV>([&](auto ic) { w[decltype(ic)::value] = io.w_codes(0, decltype(ic)::value); });
   static_for<MR>([&](auto jc) {
     x[0][decltype(jc)::value] = io.x_frag(0, 0, decltype(jc)::value);
@@ -410,29 +440,34 @@ __device__ __forceinline__ void q8_spread3(const LmheadArgs& a, int v0, int v_en
   int slot = 0;
   for (int k = 0; k < KT; ++k) {
     const int nslot = slot == NST - 1 ? 0 : slot + 1;
-    uint32_t wa = 0, wb = 0;
+    const int free_slot = slot == 0 ? NST - 1 : slot - 1;      // of stages k - 1 and k + 2
     const int kn = min(k + 1, KT - 1);
+    uint32_t wa = 0, wb = 0;
     static_for<NM>([&](auto mc) {
       constexpr int m = decltype(mc)::value;
       constexpr int s = m / (MV * MR), q = m % (MV * MR), i = q / MR, j = q % MR;
-      constexpr int b = s * MV + i, nb_ = (b + 1) % (NS * MV), ns = nb_ / MV, ni = nb_ % MV;
-      acc[i][j] = Mfma16::mma(
-          __builtin_bit_cast(bf16x8, make_uint4(f[b & 1][0], f[b & 1][1], f[b & 1][2], f[b & 1][3])),
-          x[s][j], acc[i][j]);
+      constexpr int b = s * MV + i, bn = (b + 1) % (NS * MV), ns = bn / MV, ni = bn % MV;
+      const bf16x8 fw = __builtin_bit_cast(
+          bf16x8, make_uint4(f[b & 1][0], f[b & 1][1], f[b & 1][2], f[b & 1][3]));
+      // pinned in the last step only (see mma_chained)
+      if constexpr (s == NS - 1) acc[i][j] = Mfma16::mma(fw, x[s][j], acc[i][j]);
+      else acc[i][j] = Mfma16::mma_chained(fw, x[s][j], acc[i][j]);
       if constexpr (m == 0) io.step_words(kn, wa, wb);
       if constexpr (m == NM / 2) io.steps_of(kn, wa, wb, na, nb);
       if constexpr (j >= MR - 2) {
-        constexpr int h = j - (MR - 2);
         const float step = b + 1 == NS * MV ? (ni < io.split ? na : nb) : (ni < io.split ? sa : sb);
-        q8_widen_half<ns, h>(w[ni], step, f[(b + 1) & 1]);
+        q8_widen_half<ns, j - (MR - 2)>(w[ni], step, f[(b + 1) & 1]);
       }
       if constexpr (m < MR) x[1][m] = io.x_frag(slot, 1, m);
       static_for<G>([&](auto cc) {
         constexpr int c = decltype(cc)::value;
-        if constexpr (c >= n1 && Q2 + rel(c) - NM == m) issue_copy(k + 2, cc);
-        if constexpr (c < n1 && Q2 + rel(c) == m) issue_copy(k + 3, cc);
+        if constexpr (c >= n1 && Q2 + rel(c) - NM == m) issue(k + 2, free_slot, cc);
+        if constexpr (c < n1 && Q2 + rel(c) == m) issue(k + 3, slot, cc);
       });
-      if constexpr (m == Q2 - 1) wait_vm_barrier<G>();
+      if constexpr (m == Q2 - 1) {
+        if (is_w) wait_vm_barrier<GW>();
+        else wait_vm_barrier<GX>();
+      }
       if constexpr (m == Q2) w[0] = io.w_codes(nslot, 0);
       if constexpr (m > Q2 && m <= Q2 + MR) x[0][m - Q2 - 1] = io.x_frag(nslot, 0, m - Q2 - 1);
       if constexpr (m > Q2 + MR) w[m - Q2 - MR] = io.w_codes(nslot, m - Q2 - MR);
@@ -447,56 +482,79 @@ __device__ __forceinline__ void q8_spread3(const LmheadArgs& a, int v0, int v_en
   __syncthreads();
 }
 
-template <int TV, int TR, int WV, int WR, int NST, int LOOP, bool STREAM_W>
-__device__ __forceinline__ void Q8Family<TV, TR, WV, WR, NST, LOOP, STREAM_W>::logits(
+template <int TV, int TR, int NST, bool SPREAD>
+__device__ __forceinline__ void Q8Family<TV, TR, NST, SPREAD>::logits(
     const LmheadArgs& a, int v0, int v_end, int r0, uint4* smem, f32x4 (&acc)[C::MV][C::MR]) {
   // the tile's place in scalar registers, whatever the compiler computed it with: the copies'
   // buffer resources have to be
   v0 = __builtin_amdgcn_readfirstlane(v0);
   v_end = __builtin_amdgcn_readfirstlane(v_end);
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  if constexpr (LOOP == 3) q8_spread3<Q8Family>(a, v0, v_end, r0, smem, acc);
+  if constexpr (kSpread) q8_spread<Q8Family>(a, v0, v_end, r0, smem, acc);
   else q8_ring<Q8Family>(a, v0, v_end, r0, smem, acc);
 }
 
-// The logits themselves: the tiles of cut's slabs x RT row tiles, rows of `pitch` elements of T.
-template <class F, class T>
-__global__ __launch_bounds__(F::C::kThreads, 1)
-void k_lmhead_logits(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_rows, T* out,
-                     int64_t pitch) {
+// The logits themselves, `type` ASV_F32, ASV_BF16 or ASV_F16, rows `pitch` elements apart.
+struct StoreArgs {
+  void* out;
+  int64_t pitch;
+  int type;
+};
+
+template <class T, class F>
+__device__ __forceinline__ void store_tile(const StoreArgs& st, int N, int v0, int v_end, int r0,
+                                           const f32x4 (&acc)[F::C::MV][F::C::MR], float one) {
   using C = typename F::C;
-  __shared__ uint4 smem[C::kLds / 16];
-  const TileAt t = tile_at(cut, a.V, RT, RT, blk_slabs, blk_rows);
-  const int r0 = t.rt * F::TR;
-  f32x4 acc[C::MV][C::MR];
-  F::logits(a, t.v0, t.v_end, r0, smem, acc);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wv = wave % F::WV, wr = wave / F::WV;
+  T* out = static_cast<T*>(st.out);
   typedef T Tv __attribute__((__vector_size__(4 * sizeof(T))));
-  const bool wide = pitch % 4 == 0 && reinterpret_cast<uintptr_t>(out) % sizeof(Tv) == 0;
-  const float one = opaque_one();
+  const bool wide = st.pitch % 4 == 0 && reinterpret_cast<uintptr_t>(out) % sizeof(Tv) == 0;
   static_for<C::MR>([&](auto jc) {
     constexpr int j = decltype(jc)::value;
-    const int n = r0 + wr * C::kWaveR + 16 * j + (lane & 15);
-    T* row = out + (size_t)n * pitch;
+    const int n = r0 + (wave / F::WV) * C::kWaveR + 16 * j + (lane & 15);
+    T* row = out + (size_t)n * st.pitch;
     static_for<C::MV>([&](auto ic) {
       constexpr int i = decltype(ic)::value;
-      const int v = t.v0 + wv * C::kWaveV + 16 * i + 4 * (lane >> 4);
+      const int v = v0 + (wave % F::WV) * C::kWaveV + 16 * i + 4 * (lane >> 4);
       Tv x;
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = (T)(acc[i][j][e] * one);
-      if (n >= a.N) return;
-      if (wide && v + 4 <= t.v_end) {
+      if (n >= N) return;
+      if (wide && v + 4 <= v_end) {
         *reinterpret_cast<Tv*>(row + v) = x;
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (v + e < t.v_end) row[v + e] = x[e];
+          if (v + e < v_end) row[v + e] = x[e];
       }
     });
     __builtin_amdgcn_sched_barrier(0);
   });
+}
+
+template <class F>
+__device__ __forceinline__ void logits_block(const LmheadArgs& a, const StoreArgs& st, int v0,
+                                             int v_end, int r0, uint4* smem) {
+  f32x4 acc[F::C::MV][F::C::MR];
+  F::logits(a, v0, v_end, r0, smem, acc);
+  const float one = opaque_one();
+  if (st.type == ASV_F32) store_tile<float, F>(st, a.N, v0, v_end, r0, acc, one);
+  else if (st.type == ASV_BF16) store_tile<__bf16, F>(st, a.N, v0, v_end, r0, acc, one);
+  else store_tile<_Float16, F>(st, a.N, v0, v_end, r0, acc, one);
+}
+
+// The tiles of cut's slabs x RT row tiles on family M, its tail's on family T.
+template <class M, class T>
+__global__ __launch_bounds__(M::C::kThreads, 1)
+void k_lmhead_logits(LmheadArgs a, SlabCut cut, int RT, int blk_slabs, int blk_rows, StoreArgs st) {
+  static_assert(M::TR == T::TR, "one row cut");
+  __shared__ uint4 smem[(M::C::kLds > T::C::kLds ? M::C::kLds : T::C::kLds) / 16];
+  const TileAt t = tile_at(cut, a.V, RT, RT, blk_slabs, blk_rows);
+  if constexpr (!std::is_same_v<M, T>) {
+    if (t.tail) return logits_block<T>(a, st, t.v0, t.v_end, t.rt * T::TR, smem);
+  }
+  logits_block<M>(a, st, t.v0, t.v_end, t.rt * M::TR, smem);
 }
 
 }  // namespace asv
