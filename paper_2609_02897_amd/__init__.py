@@ -8,6 +8,7 @@ device pointers and torch's current HIP stream through ctypes. There is no CPU f
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from typing import NamedTuple, Optional
 
@@ -58,6 +59,16 @@ def make_params(alpha: float = 0.3, rar0: float = 1.0, breaker_n: int = 5,
 def _check(code: int):
     if code != ASV_OK:
         raise AsvError(code)
+
+
+def _on(device):
+    """A context in which `device` is the current one: the library launches on the current device. Costs
+    next to nothing where it is already."""
+    import torch
+    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+_HERE = contextlib.nullcontext()
 
 
 def _stream_handle(device) -> int:
@@ -229,7 +240,7 @@ def quantize_lm_head(w_lm) -> PackedLmHead:
     V, H = w_lm.shape
     _need(w_lm, "weight", torch.bfloat16, (V, H))
     data = torch.empty(packed_lm_head_bytes(V, H, "fp8"), dtype=torch.uint8, device=w_lm.device)
-    with torch.cuda.device(w_lm.device):
+    with _on(w_lm.device):
         _check(load().asv_quantize_lm_head(w_lm.data_ptr(), V, H, data.data_ptr(), data.numel(),
                                            _stream_handle(w_lm.device)))
     return PackedLmHead(data, V, H, "fp8")
@@ -248,7 +259,7 @@ def pack_lm_head_fp8(q, scale) -> PackedLmHead:
     if scale.device != q.device:
         raise ValueError(f"scale: on {scale.device}, the codes are on {q.device}")
     data = torch.empty(packed_lm_head_bytes(V, H, "fp8"), dtype=torch.uint8, device=q.device)
-    with torch.cuda.device(q.device):
+    with _on(q.device):
         _check(load().asv_pack_fp8_lm_head(q.data_ptr(), scale.data_ptr(), V, H, data.data_ptr(),
                                            data.numel(), _stream_handle(q.device)))
     return PackedLmHead(data, V, H, "fp8")
@@ -344,7 +355,7 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
     lib = load()
     if ruled:
         r = _rules(rules, B, N, V, dev)
-        with torch.cuda.device(dev):
+        with _on(dev):
             _check(lib.asv_verify_ruled(ctypes.byref(a), ctypes.byref(r), workspace.data_ptr(),
                                         workspace.numel(), _stream_handle(dev)))
     elif noalloc:
@@ -380,23 +391,32 @@ def _rules(rules: Optional[LogitRules], B: int, N: int, V: int, device) -> AsvLo
     r = AsvLogitRules()
     if rules is None:
         return r
+    counts, repetition, presence, frequency, bias, allowed = rules
     f32, i32 = torch.float32, torch.int32
-    for name, dtype, shape in (("counts", i32, (B, V)), ("repetition", f32, (B,)),
-                               ("presence", f32, (B,)), ("frequency", f32, (B,)),
-                               ("allowed", i32, (N, -(-V // 32)))):
-        t = getattr(rules, name)
-        if t is not None:
-            _need(t, f"rules.{name}", dtype, shape)
-            setattr(r, name, t.data_ptr())
-    t = rules.bias
-    if t is not None:
-        if isinstance(t, torch.Tensor) and t.dim() == 2:
-            r.bias_pitch = _need_rows(t, "rules.bias", f32, (B, V))
+    if counts is not None:
+        _need(counts, "rules.counts", i32, (B, V))
+        r.counts = counts.data_ptr()
+    if repetition is not None:
+        _need(repetition, "rules.repetition", f32, (B,))
+        r.repetition = repetition.data_ptr()
+    if presence is not None:
+        _need(presence, "rules.presence", f32, (B,))
+        r.presence = presence.data_ptr()
+    if frequency is not None:
+        _need(frequency, "rules.frequency", f32, (B,))
+        r.frequency = frequency.data_ptr()
+    if bias is not None:
+        if isinstance(bias, torch.Tensor) and bias.dim() == 2:
+            r.bias_pitch = _need_rows(bias, "rules.bias", f32, (B, V))
         else:
-            _need(t, "rules.bias", f32, (V,))
-        r.bias = t.data_ptr()
-    for name, t in zip(rules._fields, rules):
+            _need(bias, "rules.bias", f32, (V,))
+        r.bias = bias.data_ptr()
+    if allowed is not None:
+        _need(allowed, "rules.allowed", i32, (N, -(-V // 32)))
+        r.allowed = allowed.data_ptr()
+    for t in rules:
         if t is not None and t.device != device:
+            name = next(n for n, x in zip(rules._fields, rules) if x is t)
             raise ValueError(f"rules.{name}: on {t.device}, the rows are on {device}")
     return r
 
@@ -460,7 +480,7 @@ def lm_head_logits(hidden, w_lm: PackedLmHead, dtype=None, out=None, workspace=N
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
     else:
         _need_workspace(workspace, need, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         _check(load().asv_lm_head_logits(ctypes.byref(a), workspace.data_ptr(), workspace.numel(),
                                          _stream_handle(dev)))
     return out
@@ -498,7 +518,7 @@ def adjust_logits(logits, rules: LogitRules, req_offsets=None, parent=None, draf
             raise ValueError(f"{name}: on {t.device}, the logits are on {dev}")
     a.in_, a.out = logits.data_ptr(), out.data_ptr()
     a.rules = _rules(rules, B, N, V, dev)
-    with torch.cuda.device(dev):
+    with _on(dev):
         _check(load().asv_adjust_logits(ctypes.byref(a), _stream_handle(dev)))
     return out
 
@@ -528,7 +548,7 @@ def token_counts(tokens, offsets, V: int, prompt_len=None, counts=None):
     status = torch.empty(B, dtype=torch.int32, device=dev)
     a.tok, a.tok_offsets = tokens.data_ptr(), offsets.data_ptr()
     a.counts, a.req_status = counts.data_ptr(), status.data_ptr()
-    with torch.cuda.device(dev):
+    with _on(dev):
         _check(load().asv_token_counts(ctypes.byref(a), _stream_handle(dev)))
     return counts, status
 

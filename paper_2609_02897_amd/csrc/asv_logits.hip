@@ -340,8 +340,11 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
       (reinterpret_cast<uintptr_t>(a->in) | reinterpret_cast<uintptr_t>(a->out)) % eb)
     return ASV_EINVAL;
   const int ids = kAdjThreads * (int)(16 / eb);
-  const int64_t grid =
-      (int64_t)((a->V + ids - 1) / ids) * ((a->N + kAdjRows - 1) / kAdjRows);
+  // fewer rows a workgroup where that takes more workgroups to fill the chip: eight of them a CU
+  const int64_t chunks = (a->V + ids - 1) / ids;
+  int rows = kAdjRows;
+  while (rows > 1 && chunks * ((a->N + rows - 1) / rows) < 8 * (int64_t)cu_count()) rows /= 2;
+  const int64_t grid = chunks * ((a->N + rows - 1) / rows);
   if (grid > INT32_MAX) return ASV_EINVAL;
   // out is in, or apart from it
   if (a->in == a->out ? a->in_pitch != a->out_pitch
@@ -352,7 +355,7 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
   (void)hipGetLastError();
   const AdjustArgs g{rule_args(a->rules, a->V), a->in,     a->out,       a->in_pitch, a->out_pitch,
                      a->req_offsets,            a->parent, a->draft_tok, a->B,        a->N,
-                     a->V};
+                     a->V,                      rows};
   switch (a->type) {
     case ASV_F32: launch_adjust<float, 4>(g, grid, s); break;
     case ASV_BF16: launch_adjust<__bf16, 8>(g, grid, s); break;
@@ -365,13 +368,17 @@ extern "C" int asv_token_counts(const asv_counts_args* a, void* stream) {
   if (!a || a->B < 0 || a->T < 0 || a->V <= 0 || a->V >= (1 << 30) || (a->add != 0 && a->add != 1))
     return ASV_EINVAL;
   if (a->B == 0) return ASV_OK;
-  const int64_t grid = (int64_t)((a->V + kCountIds - 1) / kCountIds) * a->B;
+  // two workgroups a CU, of at least kCountLeast ids and at most what the LDS holds
+  const int64_t want = std::max<int64_t>(1, 2 * (int64_t)cu_count() / a->B);
+  const int64_t share = ((int64_t)a->V + want - 1) / want;
+  const int ids = (int)std::min<int64_t>(kCountIds, std::max<int64_t>(kCountLeast, (share + 3) / 4 * 4));
+  const int64_t grid = ((int64_t)a->V + ids - 1) / ids * a->B;
   if ((!a->tok && a->T > 0) || !a->tok_offsets || !a->counts || !a->req_status || grid > INT32_MAX)
     return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();
   const CountArgs g{a->tok, a->tok_offsets, a->prompt_len, a->T,     a->B,
-                    a->V,   a->add,         a->counts,     a->req_status};
+                    a->V,   a->add,         ids,           a->counts, a->req_status};
   k_token_counts<<<(unsigned)grid, kCountThreads, 0, s>>>(g);
   return launch_status("k_token_counts");
 }

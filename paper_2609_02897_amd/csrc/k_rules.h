@@ -164,18 +164,25 @@ struct RuleRows {
   }
 };
 
-// Four consecutive entries of a [..][V] row from id v on (a multiple of 4), 0 past V.
-template <class T4, class T>
-__device__ __forceinline__ T4 load4(const T* __restrict__ row, int v, int V, bool wide) {
-  T4 x = {};
-  if (wide) {
-    if (v < V) x = *reinterpret_cast<const T4*>(row + v);
+// PT entries of an array from entry `at` on, those past `left` as the last one; zeros without an array.
+template <int PT, class T>
+__device__ __forceinline__ void load_row(const T* __restrict__ p, size_t at, int left, bool wide,
+                                         T (&x)[PT]) {
+  typedef T T4 __attribute__((__vector_size__(16)));
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < PT; ++e) x[e] = T(0);
+  } else if (wide) {
+#pragma unroll
+    for (int q = 0; q < PT; q += 4) {
+      const T4 y = *reinterpret_cast<const T4*>(p + at + q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[q + e] = y[e];
+    }
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (v + e < V) x[e] = row[v + e];
+    for (int e = 0; e < PT; ++e) x[e] = p[at + min(e, left - 1)];
   }
-  return x;
 }
 
 typedef int i32x4 __attribute__((__vector_size__(16)));
@@ -444,14 +451,8 @@ struct TileRules {
 
 // ---- the rules on logits in memory (K11)
 
-template <class T>
-__device__ __forceinline__ float to_f32(T x) {
-  if constexpr (std::is_same_v<T, float>) return x;
-  else return (float)x;
-}
-
 constexpr int kAdjThreads = 256;
-constexpr int kAdjRows = 8;           // rows of a workgroup
+constexpr int kAdjRows = 8;           // most rows of a workgroup
 
 struct AdjustArgs {
   RuleArgs r;
@@ -462,68 +463,58 @@ struct AdjustArgs {
   const int32_t* parent;
   const int32_t* draft_tok;
   int B, N, V;
+  int rows;                           // of a workgroup, at most kAdjRows
 };
 
-// Grid ceil(V / kIds) * ceil(N / kAdjRows), the ids fastest: the workgroup takes kIds ids of its rows, each thread
-// PT consecutive ones (16 bytes of input). Memory bound: one read and one write of the logits; the
-// rows of one request read the table and the bias once, into registers.
+// Grid ceil(V / kIds) * ceil(N / rows), the ids fastest: the workgroup takes kIds ids of its rows, each
+// thread PT consecutive ones (16 bytes of input). Memory bound: one read and one write of the logits; the
+// table and the bias are read once for the consecutive rows of one request. Many waves with one row under
+// way each: 2048 rows of 128256 fp32 logits 494 us at 8 rows (4.4 TB/s; a copy of 2 GB on the same box 4.9),
+// 513 at 4, 511 at 16; with two and four rows' loads issued together 527 and 611.
 template <class T, int PT>
 __global__ __launch_bounds__(kAdjThreads)
 void k_adjust(AdjustArgs a) {
   constexpr int kIds = kAdjThreads * PT;
   __shared__ RuleRows<kAdjRows> rows;
   const int chunks = (a.V + kIds - 1) / kIds, group = blockIdx.x / chunks;
-  const int tid = threadIdx.x, r0 = group * kAdjRows, v0 = (blockIdx.x - group * chunks) * kIds;
-  const int v_end = min(v0 + kIds, a.V), r_end = min(r0 + kAdjRows, a.N);
-  rows.template build<kAdjThreads>(a.r, a.off, a.parent, a.draft_tok, a.B, a.N, r0, v0, v_end,
+  const int tid = threadIdx.x, r0 = group * a.rows, v0 = (blockIdx.x - group * chunks) * kIds;
+  const int v_end = min(v0 + kIds, a.V), r_end = min(r0 + a.rows, a.N);
+  rows.template build<kAdjThreads>(a.r, a.off, a.parent, a.draft_tok, a.B, r_end, r0, v0, v_end,
                                    NoPrefetch{});
   const bool hit = __builtin_amdgcn_readfirstlane(rows.hit);
   const int v = v0 + tid * PT;
   if (v >= v_end) return;
   const RuleArgs& r = a.r;
   const int V = a.V;
-  const bool wide_c = (V & 3) == 0 && (reinterpret_cast<uintptr_t>(r.counts) & 15) == 0;
-  const bool wide_b = (r.bias_pitch & 3) == 0 && (V & 3) == 0 &&
-                      (reinterpret_cast<uintptr_t>(r.bias) & 15) == 0;
+  const bool full = v + PT <= V;
+  const bool wide_c = full && V % 4 == 0 && reinterpret_cast<uintptr_t>(r.counts) % 16 == 0;
+  const bool wide_b = full && r.bias_pitch % 4 == 0 && reinterpret_cast<uintptr_t>(r.bias) % 16 == 0;
   const T* in = static_cast<const T*>(a.in);
   T* out = static_cast<T*>(a.out);
-  const bool wide_in = a.in_pitch % PT == 0 && (reinterpret_cast<uintptr_t>(in) & 15) == 0 &&
-                       v + PT <= V;
-  const bool wide_out = a.out_pitch % PT == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 &&
-                        v + PT <= V;
+  const bool wide_in = full && a.in_pitch % PT == 0 && reinterpret_cast<uintptr_t>(in) % 16 == 0;
+  const bool wide_out = full && a.out_pitch % PT == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
   typedef T Tv __attribute__((__vector_size__(PT * sizeof(T))));
   int cur = -1;
-  int c[PT];
-  float bias[PT];
+  int c[PT] = {};
+  float bias[PT] = {};
   for (int n = r0; n < r_end; ++n) {
-    const int i = n - r0, b = rows.req(i);
-    float z[PT];
+    const int i = n - r0, b = __builtin_amdgcn_readfirstlane(rows.req(i));
+    const T* from = in + (size_t)n * a.in_pitch + v;
+    Tv x;
     if (wide_in) {
-      const Tv x = *reinterpret_cast<const Tv*>(in + (size_t)n * a.in_pitch + v);
-#pragma unroll
-      for (int e = 0; e < PT; ++e) z[e] = to_f32<T>(x[e]);
+      x = *reinterpret_cast<const Tv*>(from);
     } else {
 #pragma unroll
-      for (int e = 0; e < PT; ++e)
-        z[e] = v + e < V ? to_f32<T>(in[(size_t)n * a.in_pitch + v + e]) : 0.f;
+      for (int e = 0; e < PT; ++e) x[e] = from[min(e, V - 1 - v)];
     }
-    uint32_t bits = ~0u;
+    const uint32_t bits =
+        r.allowed ? r.allowed[(size_t)n * r.words + (v >> 5)] >> (v & 31) : ~0u;
+    float z[PT];
     if (b >= 0) {
-      if (r.allowed) bits = r.allowed[(size_t)n * r.words + (v >> 5)] >> (v & 31);
       if (b != cur) {
         cur = b;
-#pragma unroll
-        for (int q = 0; q < PT; q += 4) {
-          const i32x4 cc = r.counts ? load4<i32x4>(r.counts + (size_t)b * V, v + q, V, wide_c)
-                                    : i32x4{};
-          const fx4 bb = r.bias ? load4<fx4>(r.bias + (size_t)b * r.bias_pitch, v + q, V, wide_b)
-                                : fx4{};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            c[q + e] = cc[e];
-            bias[q + e] = bb[e];
-          }
-        }
+        load_row<PT>(r.counts, (size_t)b * V + v, V - v, wide_c, c);
+        load_row<PT>(r.bias, (size_t)b * r.bias_pitch + v, V - v, wide_b, bias);
       }
       const RowRule rr = rows.rule(i, r0);
       int path[PT] = {};
@@ -532,30 +523,40 @@ void k_adjust(AdjustArgs a) {
 #pragma unroll
           for (int e = 0; e < PT; ++e) path[e] += d == v + e;
         });
+      int any = 0;
 #pragma unroll
       for (int e = 0; e < PT; ++e) {
-        if (c[e] != 0 || path[e] != 0) z[e] = penalised(z[e], c[e], path[e], rr);
+        z[e] = (float)x[e];
+        any |= c[e] | path[e];
+      }
+      if (any != 0) {
+#pragma unroll
+        for (int e = 0; e < PT; ++e) z[e] = penalised(z[e], c[e], path[e], rr);
+      }
+#pragma unroll
+      for (int e = 0; e < PT; ++e) {
         if (r.bias) z[e] = __fadd_rn(z[e], bias[e]);
         z[e] = (bits >> e) & 1 ? z[e] : kNegInf;
+        x[e] = (T)z[e];
       }
     }
+    T* to = out + (size_t)n * a.out_pitch + v;
     if (wide_out) {
-      Tv x;
-#pragma unroll
-      for (int e = 0; e < PT; ++e) x[e] = (T)z[e];
-      *reinterpret_cast<Tv*>(out + (size_t)n * a.out_pitch + v) = x;
+      *reinterpret_cast<Tv*>(to) = x;
     } else {
 #pragma unroll
       for (int e = 0; e < PT; ++e)
-        if (v + e < V) out[(size_t)n * a.out_pitch + v + e] = (T)z[e];
+        if (v + e < V) to[e] = x[e];
     }
   }
 }
 
 // ---- the history table (K10)
 
-constexpr int kCountThreads = 256;
-constexpr int kCountIds = 8192;       // ids of a workgroup, 32 KB of LDS
+constexpr int kCountThreads = 1024;
+constexpr int kCountIds = 20480;      // most ids of a workgroup, 80 KB of LDS: two workgroups a CU
+constexpr int kCountLeast = 1024;     // fewest, where there are more
+constexpr int kCountBatch = 8;        // tokens of a thread whose loads are issued together
 
 struct CountArgs {
   const int32_t* tok;                 // [T]
@@ -563,19 +564,23 @@ struct CountArgs {
   const int32_t* prompt;              // [B] or null
   int T, B, V;
   int add;
+  int ids;                            // of a workgroup, a multiple of 4
   int32_t* counts;
   int32_t* status;
 };
 
-// Grid ceil(V / kCountIds) * B: the workgroup counts its ids of request b in LDS over all of the
+// Grid ceil(V / ids) * B: the workgroup counts its ids of request b in LDS over all of the
 // request's tokens and writes (or adds) its part of the table: no fill, and every count is the sum
-// of integers, the same in any order. Tokens outside [0, V) are passed over and reported.
+// of integers, the same in any order. Tokens outside [0, V) are passed over and reported. A long list is
+// a chain of loads, so each thread has kCountBatch of them under way, and as few workgroups as fill the
+// chip read it. 64 lists of up to 14000 tokens at V = 151936, whose table takes 6 us to write: one load at a
+// time and 8192 ids a workgroup 31.5 us, eight at a time 19.9, two workgroups a CU 18.2.
 static __global__ __launch_bounds__(kCountThreads)
 void k_token_counts(CountArgs a) {
-  __shared__ int s_n[kCountIds];
-  const int chunks = (a.V + kCountIds - 1) / kCountIds, b = blockIdx.x / chunks;
-  const int v0 = (blockIdx.x - b * chunks) * kCountIds, tid = threadIdx.x;
-  const int ids = min(kCountIds, a.V - v0);
+  __shared__ __attribute__((aligned(16))) int s_n[kCountIds];
+  const int chunks = (a.V + a.ids - 1) / a.ids, b = blockIdx.x / chunks;
+  const int v0 = (blockIdx.x - b * chunks) * a.ids, tid = threadIdx.x;
+  const int ids = min(a.ids, a.V - v0);
   int lo = a.off[b], hi = a.off[b + 1], bad = 0;
   if (lo < 0 || hi < lo || hi > a.T) {
     bad = ASV_RS_BAD_OFFSETS;
@@ -585,23 +590,37 @@ void k_token_counts(CountArgs a) {
   for (int i = tid; i < ids; i += kCountThreads) s_n[i] = 0;
   __syncthreads();
   bool out = false;
-  for (int t = lo + tid; t < hi; t += kCountThreads) {
-    const int v = a.tok[t];
-    out |= v < 0 || v >= a.V;
-    if (v < v0 || v >= v0 + ids) continue;
-    if (t - lo < n_prompt) atomicOr(&s_n[v - v0], ASV_COUNT_PROMPT);
-    else atomicAdd(&s_n[v - v0], 1);
+  for (int64_t t0 = lo + tid; t0 < hi; t0 += kCountBatch * kCountThreads) {
+    int tok[kCountBatch];
+#pragma unroll
+    for (int u = 0; u < kCountBatch; ++u)
+      tok[u] = a.tok[min(t0 + u * kCountThreads, (int64_t)hi - 1)];
+#pragma unroll
+    for (int u = 0; u < kCountBatch; ++u) {
+      const int64_t t = t0 + u * kCountThreads;
+      const int v = tok[u];
+      if (t >= hi) break;
+      out |= v < 0 || v >= a.V;
+      if (v < v0 || v >= v0 + ids) continue;
+      if (t - lo < n_prompt) atomicOr(&s_n[v - v0], ASV_COUNT_PROMPT);
+      else atomicAdd(&s_n[v - v0], 1);
+    }
   }
   bad |= __syncthreads_or(out) ? ASV_RS_BAD_TOKEN : 0;
   if (tid == 0 && v0 == 0) a.status[b] = bad;
   int32_t* row = a.counts + (size_t)b * a.V + v0;
-  for (int i = tid; i < ids; i += kCountThreads) {
-    const int c = s_n[i];
-    if (!a.add) row[i] = c;
-    else if (c != 0) {
+  if (a.add) {
+    for (int i = tid; i < ids; i += kCountThreads) {
+      const int c = s_n[i];
+      if (c == 0) continue;
       const int old = row[i];
       row[i] = ((old & kCountMask) + (c & kCountMask)) | ((old | c) & ASV_COUNT_PROMPT);
     }
+  } else if (a.V % 4 == 0 && reinterpret_cast<uintptr_t>(a.counts) % 16 == 0) {
+    for (int i = 4 * tid; i < ids; i += 4 * kCountThreads)
+      *reinterpret_cast<int4*>(row + i) = *reinterpret_cast<const int4*>(&s_n[i]);
+  } else {
+    for (int i = tid; i < ids; i += kCountThreads) row[i] = s_n[i];
   }
 }
 
