@@ -96,29 +96,43 @@ size_t q8_max_records(int N, int V) {
 struct Q8Plan {
   int rows;          // tile rows: 64, 128, 192 or 256
   int ids;           // 64 rows: ids of the tile; else ids of the tail's tile
+  int tail;          // 64 rows: ids of the tail's tile, 0 without a tail
   SlabCut cut;
   int S;             // slabs in all
   int64_t est;       // beyond 64 rows
 };
 
-// Up to 64 rows, in us at 60 rows and H = 4096 on weights that are not in the caches (a read at 7 TB/s, the
-// rule's choice, the best of 24 others): V = 8000 5, 25, 25; 16000 9, 25, 25; 24000 14, 31, 31; 32000
-// 19, 34, 31; 40000 23, 39, 39; 50000 29, 43, 43; 64000 37, 48, 47; 80000 47, 65, 63; 100000 59, 69, 69;
-// 128256 75, 81, 81; 140000 82, 106, 106; 151936 89, 113, 113; 200000 117, 140, 138; 260000 152, 159, 159.
+// Up to 64 rows: equal slabs, two or three a CU, where the tile that holds them has little left over; else whole
+// tiles, as many on every CU, and a tail of one or two narrower ones each, which start as the first of the
+// whole ones end. us of 57 rows' bf16 logits at H = 4096 on weights that are not in the caches (what they
+// move at 7 TB/s, this rule, equal slabs only): V = 16000 10, 28; 32000 19, 35; 40000 24, 38, 44; 50000 30,
+// 46; 64000 38, 52; 80000 48, 66, 69; 100000 60, 75; 128256 77, 85; 140000 84, 97, 120; 151936 91, 101, 128;
+// 180000 108, 124, 154; 200000 120, 142, 161; 260000 156, 186, 196.
 Q8Plan q8_rows64(int V, int cus) {
+  const int64_t c = cus;
   auto even = [&](int ids, int width) {
     const int S = (V + width - 1) / width;
-    return Q8Plan{64, ids, SlabCut{S, width, width, 0, 0}, S, 0};
+    return Q8Plan{64, ids, 0, SlabCut{S, width, width, 0, 0}, S, 0};
   };
-  const int64_t c = cus;
+  auto tailed = [&](int ids, int64_t a_cu, int width) {
+    const int n_main = (int)(a_cu * c), S = n_main + (V - n_main * ids + width - 1) / width;
+    return Q8Plan{64, ids, width <= 64 ? 64 : 128, SlabCut{n_main, ids, width, 0, 0}, S, 0};
+  };
   const int two = q8_share(V, 2 * c);
   if (V <= c * 64) return even(64, 64);
   if (two <= 64) return even(64, two);
-  if (two <= 128) return even(128, two);
+  for (int a_cu = 1; a_cu <= 2; ++a_cu) {
+    if (V <= c * 128 * a_cu) return even(128, two);
+    const int width = q8_share(V - c * 128 * a_cu, c);
+    if (width <= 64) return tailed(128, a_cu, width);
+  }
   if (two <= 256) return even(256, two);
-  if (V <= 3 * c * 256) return even(128, 128);
-  // whole pairs of shares, which a CU runs side by side
-  return even(256, q8_share(V, 2 * c * ((V + 512 * c - 1) / (512 * c))));
+  const int three = q8_share(V, 3 * c);
+  if (three > 224 && three <= 256) return even(256, three);
+  const int64_t a_cu = V / (c * 256), rest = V - a_cu * c * 256;
+  if (rest == 0) return even(256, 256);
+  const int width = q8_share(rest, c);
+  return tailed(256, a_cu, width <= 128 ? width : q8_share(rest, 2 * c));
 }
 
 // Beyond: whole rounds of 256-id tiles and a tail of one narrower tile a CU, where that is estimated to
@@ -139,7 +153,7 @@ Q8Plan q8_tail_plan(int N, int V, int cus, int64_t plan_est) {
     const int ids = width <= 64 ? 64 : 128;
     const int64_t tail = ids == 64 ? f.tail64 : f.tail128, est = rounds * f.cost + tail;
     if (tail == INT32_MAX || est >= best.est) continue;
-    best = Q8Plan{f.rows, ids, SlabCut{n_main, kSlab, width, 0, 0},
+    best = Q8Plan{f.rows, ids, 0, SlabCut{n_main, kSlab, width, 0, 0},
                   n_main + n_tail, est};
   }
   return best;
@@ -153,11 +167,11 @@ int q8_launches(int N, int V, int cus, Fn&& f) {
   if (N <= 64) {
     const Q8Plan p = q8_rows64(V, cus);
     k.row_tiles = 1;
-    switch (p.ids) {
-      case 64: f(Q8Ids64{}, Q8Ids64{}, p.cut, 0, k); break;
-      case 128: f(Q8Ids128{}, Q8Ids128{}, p.cut, 0, k); break;
-      default: f(Q8Ids256{}, Q8Ids256{}, p.cut, 0, k); break;
-    }
+    const int tail = p.tail ? p.S - p.cut.n_main : 0;
+    if (p.ids == 64) f(Q8Ids64{}, Q8Ids64{}, p.cut, 0, k);
+    else if (p.ids == 128) f(Q8Ids128{}, Q8Ids64{}, p.cut, tail, k);
+    else if (p.tail == 128) f(Q8Ids256{}, Q8Ids128{}, p.cut, tail, k);
+    else f(Q8Ids256{}, Q8Ids64{}, p.cut, tail, k);
     return p.S;
   }
   const int S = (V + kSlab - 1) / kSlab;

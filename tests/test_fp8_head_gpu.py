@@ -64,7 +64,8 @@ SHAPES = [(1, 1, 64), (1, 257, 128), (3, 5, 64), (16, 127, 192), (17, 128, 576),
           (64, 255, 4096), (65, 256, 128), (128, 513, 192), (129, 300, 256), (193, 1025, 64),
           (257, 129, 448), (300, 700, 320), (2, 33, 4160), (5, 260, 8320), (130, 270, 8256),
           # every cut of the ids: 64-, 128- and 256-id tiles, tails of 64 and 128 ids behind rounds
-          (7, 20001, 64), (60, 40003, 64), (33, 70001, 64), (3, 140001, 64), (2, 200001, 64),
+          (7, 20001, 64), (60, 40003, 64), (64, 50001, 64), (33, 70001, 64), (9, 90001, 64),
+          (3, 140001, 64), (4, 152001, 64), (5, 168003, 64), (6, 180003, 64), (2, 200001, 64),
           (100, 32000, 64), (90, 75003, 64), (190, 20000, 64), (333, 40003, 128), (150, 36003, 64),
           (500, 18000, 64), (230, 67003, 64)]
 
