@@ -437,6 +437,8 @@ typedef struct asv_counts_args {
                                      request counts as empty) */
 } asv_counts_args;
 
+/* Write the table or add to it. ASV_EINVAL for bad sizes or null or misaligned pointers, ASV_EHIP if the
+ * launch fails. */
 int asv_token_counts(const asv_counts_args *args, void *stream);
 
 /* ---- For callers that cannot allocate device memory (code under HIP graph capture, tight

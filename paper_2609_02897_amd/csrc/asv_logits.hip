@@ -227,12 +227,13 @@ int verify_fp8(const asv_verify_args* a, char* ws, hipStream_t s, const E& e) {
 
 // ---- rules
 
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+template <class... P>
+bool aligned4(const P*... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0;
+}
 
 bool rules_ok(const asv_logit_rules& r, int V) {
-  for (const void* p : {(const void*)r.counts, (const void*)r.repetition, (const void*)r.presence,
-                        (const void*)r.frequency, (const void*)r.bias, (const void*)r.allowed})
-    if (!aligned4(p)) return false;
+  if (!aligned4(r.counts, r.repetition, r.presence, r.frequency, r.bias, r.allowed)) return false;
   return !r.bias || r.bias_pitch == 0 || r.bias_pitch >= V;
 }
 
@@ -351,6 +352,7 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
   if (a->B == 0) return ASV_OK;
   const size_t eb = element_bytes(a->type);
   if (!a->in || !a->out || a->in_pitch < a->V || a->out_pitch < a->V ||
+      !aligned4(a->req_offsets, a->parent, a->draft_tok) ||
       (reinterpret_cast<uintptr_t>(a->in) | reinterpret_cast<uintptr_t>(a->out)) % eb)
     return ASV_EINVAL;
   const int ids = kAdjThreads * (int)(16 / eb);
@@ -387,7 +389,8 @@ extern "C" int asv_token_counts(const asv_counts_args* a, void* stream) {
   const int64_t share = ((int64_t)a->V + want - 1) / want;
   const int ids = (int)std::min<int64_t>(kCountIds, std::max<int64_t>(kCountLeast, (share + 3) / 4 * 4));
   const int64_t grid = ((int64_t)a->V + ids - 1) / ids * a->B;
-  if ((!a->tok && a->T > 0) || !a->tok_offsets || !a->counts || !a->req_status || grid > INT32_MAX)
+  if ((!a->tok && a->T > 0) || !a->tok_offsets || !a->counts || !a->req_status || grid > INT32_MAX ||
+      !aligned4(a->tok, a->tok_offsets, a->prompt_len, a->counts, a->req_status))
     return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();

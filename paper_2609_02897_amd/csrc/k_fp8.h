@@ -26,8 +26,6 @@
 namespace asv {
 
 constexpr int kQBlock = 128;          // columns (and ids of W) of one scale
-typedef int i32x8 __attribute__((__vector_size__(32)));
-typedef __bf16 bf16x2 __attribute__((__vector_size__(4)));
 
 __host__ __device__ __forceinline__ int q8_blocks(int H) { return (H + kQBlock - 1) / kQBlock; }
 // scale bytes of a row of blocks: whole 32-bit words

@@ -590,7 +590,7 @@ void k_token_counts(CountArgs a) {
   for (int i = tid; i < ids; i += kCountThreads) s_n[i] = 0;
   __syncthreads();
   bool out = false;
-  for (int64_t t0 = lo + tid; t0 < hi; t0 += kCountBatch * kCountThreads) {
+  for (int64_t t0 = (int64_t)lo + tid; t0 < hi; t0 += kCountBatch * kCountThreads) {
     int tok[kCountBatch];
 #pragma unroll
     for (int u = 0; u < kCountBatch; ++u)
