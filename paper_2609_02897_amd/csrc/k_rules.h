@@ -79,7 +79,7 @@ struct RuleRows {
   int2 at[TR];                 // request and its first row
   RowRule rules[TR];           // of the request that starts, or goes on, at this row
   int seg_lo, hit;
-  int tok[kPathStage], par[kPathStage];
+  int2 node[kPathStage];       // link and token
 
   // All threads of the workgroup, T of them; draft_tok null: no paths, off null: row n is request n. `pre`:
   // what the thread has loaded beforehand (NoPrefetch: nothing).
@@ -103,14 +103,29 @@ struct RuleRows {
     }
     for (int i = tid; i < TR; i += T) at[i] = make_int2(-1, r0);
     __syncthreads();
-    for (int b = tid; b < B; b += T) {
-      const bool known = P::kHas && b == tid;
-      const int first = known ? pre.lo : off[b];
-      const int from = max(first, r0), to = min(known ? pre.hi : off[b + 1], r_end);
-      if (first < 0 || from >= to) continue;
-      put_rule(from - r0, known ? pre.rule : row_rule(a, b));
-      for (int n = from; n < to; ++n) at[n - r0] = make_int2(b, first);
-      if (first < r0) seg_lo = first;         // the one request that starts before the rows
+    for (int b0 = 0; b0 < B; b0 += T) {
+      const int b = b0 + tid;
+      int first = -1, from = 0, to = 0;
+      if (b < B) {
+        const bool known = P::kHas && b0 == 0;
+        first = known ? pre.lo : off[b];
+        from = max(first, r0);
+        to = min(known ? pre.hi : off[b + 1], r_end);
+      }
+      const bool mine = first >= 0 && from < to, many = mine && to - from > 4;
+      if (mine) {
+        put_rule(from - r0, P::kHas && b0 == 0 ? pre.rule : row_rule(a, b));
+        if (first < r0) seg_lo = first;       // the one request that starts before the rows
+        if (!many)
+          for (int n = from; n < to; ++n) at[n - r0] = make_int2(b, first);
+      }
+      // the rows of a larger request, by its whole wave (by its thread alone: 2 us for 60 rows)
+      for (uint64_t m = __builtin_amdgcn_ballot_w64(many); m != 0; m &= m - 1) {
+        const int l = __builtin_ctzll(m);
+        const int2 x = make_int2(__builtin_amdgcn_readlane(b, l), __builtin_amdgcn_readlane(first, l));
+        const int end = __builtin_amdgcn_readlane(to, l);
+        for (int n = __builtin_amdgcn_readlane(from, l) + (tid & 63); n < end; n += kWave) at[n - r0] = x;
+      }
     }
     __syncthreads();
     if (!draft_tok) return;
@@ -118,10 +133,7 @@ struct RuleRows {
     bool any = false;
     auto put = [&](int c, int p, int d) {
       any |= d >= v0 && d < v_end;
-      if (c - base < kPathStage) {
-        tok[c - base] = d;
-        par[c - base] = p;
-      }
+      if (c - base < kPathStage) node[c - base] = make_int2(p, d);
     };
     if constexpr (P::kHas) {
       // nodes r0 + 1 .. of the rows are known; r0 is a root where no request starts before it
@@ -155,11 +167,12 @@ struct RuleRows {
     if (at[i].x < 0) return;
     const int base = seg_lo, first = at[i].y;
     for (int c = r0 + i; c > first;) {
-      const bool in = (unsigned)(c - base) < (unsigned)kPathStage;
-      const int d = in ? tok[c - base] : draft_tok[c], p = in ? par[c - base] : parent[c];
-      f(d);
-      if (p < first || p >= c) break;
-      c = p;
+      int2 x;
+      if ((unsigned)(c - base) < (unsigned)kPathStage) x = node[c - base];
+      else x = make_int2(parent[c], draft_tok[c]);
+      f(x.y);
+      if (x.x < first || x.x >= c) break;
+      c = x.x;
     }
   }
 };
@@ -327,8 +340,8 @@ struct TileRules {
   }
 
   // What a lane holds of the table and the bias for its ids, for the request of its last row, and of the
-  // mask for its next row: the rows of a block mostly belong to one request, the block before's, and
-  // the mask's words are on their way while a block is computed. Every load is from a place inside its
+  // mask for its next row: the rows of a block mostly belong to one request, the block before's. The
+  // mask's words, and another request's entries, are on their way while the block before is reduced. Every load is from a place inside its
   // array, whatever the row and the ids; what it brings of other rows and ids is masked or discarded.
   struct Held {
     int b = -2;
@@ -370,6 +383,11 @@ struct TileRules {
     h.b = b;
     h.fresh = true;
   }
+  // The request of this lane's row of block j, or where it has none another.
+  __device__ __forceinline__ int request_of(int j, int other) const {
+    const int b = rows.req(wr * C::kWaveR + 16 * j + (lane & 15));
+    return b < 0 ? other : b;
+  }
   // Ahead of the gather, which covers the loads.
   __device__ __forceinline__ void begin(Held& h) const {
     static_for<C::MV>([&](auto ic) {
@@ -382,15 +400,13 @@ struct TileRules {
         h.ids |= (uint32_t)(v0 + vw + 16 * i + e < v_end) << (4 * i + e);
     });
     load_bits(0, h.bits);
-    load_request(max(rows.req(wr * C::kWaveR + (lane & 15)), 0), h);
+    load_request(request_of(0, 0), h);
   }
 
   // Row block j through the rules, into z[4 i + e], -inf past the tile's ids; blocks in order, begin()
   // before the first. Rows of no request give no results (their offsets are malformed).
   __device__ __forceinline__ void block(int j, float (&z)[4 * C::MV], Held& h) const {
     const int i_row = wr * C::kWaveR + 16 * j + (lane & 15);
-    const int b = max(rows.req(i_row), 0);
-    if (!__all(b == h.b)) load_request(b, h);
     if (h.fresh && r.counts) {
       h.seen = 0;
       static_for<C::MV>([&](auto ic) {
@@ -439,6 +455,10 @@ struct TileRules {
         constexpr int i = decltype(ec)::value / 4, e = decltype(ec)::value % 4;
         z[4 * i + e] = __fadd_rn(z[4 * i + e], h.bias[i][e]);
       });
+    }
+    if (j + 1 < C::MR) {
+      const int b = request_of(j + 1, h.b);
+      if (!__all(b == h.b)) load_request(b, h);
     }
     // a bit of `keep` as a mask over the value: set, the value, else -inf
     static_for<4 * C::MV>([&](auto kc) {
