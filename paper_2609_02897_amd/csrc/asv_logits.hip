@@ -135,26 +135,27 @@ Q8Plan q8_rows64(int V, int cus) {
   return tailed(256, a_cu, width <= 128 ? width : q8_share(rest, 2 * c));
 }
 
-// Beyond: whole rounds of 256-id tiles and a tail of one narrower tile a CU, where that is estimated to
-// be faster than the best plan over whole slabs. Costs as K1's (its rounds are in the same proportion here:
-// 64, 77 and 97 us); a round of tails of 64 and 128 ids as K1's.
+// Up to 256 rows, in one row tile: whole rounds of 256-id tiles and a tail of one narrower tile a CU, where
+// that is estimated to be faster than the best plan over whole slabs (by K1's costs: its rounds are in the
+// same proportion here, 64, 77 and 97 us). us of bf16 logits at H = 4096 on weights that are not in the caches,
+// whole slabs -> with the tail: 100 rows, V = 16000 55 -> 40, 32000 58 -> 55, 70003 119 -> 101; 128 rows,
+// 32000 56 -> 49, 75003 127 -> 110, 90003 129 -> 125; 190 rows, 16000 56 -> 49, 67003 148 -> 140; 256 rows,
+// 14000 56 -> 48, 70003 195 -> 192. Tails of 128 ids lose at 190 rows (20000: 56 -> 65), and any behind two
+// row tiles (333 rows, 40003: 124 -> 137; 480 rows level).
 Q8Plan q8_tail_plan(int N, int V, int cus, int64_t plan_est) {
   struct Family { int rows, cost, tail64, tail128; };
-  const Family families[3] = {{128, 62, 30, 44}, {192, 80, 36, 54}, {256, 98, 44, INT32_MAX}};
+  const Family families[3] = {{128, 62, 46, 57}, {192, 80, 60, 0}, {256, 98, 80, 0}};
   Q8Plan best{};
   best.est = plan_est;
   for (const Family& f : families) {
-    const int RT = (N + f.rows - 1) / f.rows, per_round = cus / RT;
-    if (per_round < 1) continue;
-    const int64_t rounds = V / ((int64_t)kSlab * per_round);
-    const int n_main = (int)(rounds * per_round), rest = V - n_main * kSlab;
-    const int width = q8_share(rest, per_round), n_tail = (rest + width - 1) / width;
-    if (rest == 0 || width > 128 || n_tail > kMaxCutTail) continue;
-    const int ids = width <= 64 ? 64 : 128;
-    const int64_t tail = ids == 64 ? f.tail64 : f.tail128, est = rounds * f.cost + tail;
-    if (tail == INT32_MAX || est >= best.est) continue;
-    best = Q8Plan{f.rows, ids, 0, SlabCut{n_main, kSlab, width, 0, 0},
-                  n_main + n_tail, est};
+    if (N > f.rows) continue;
+    const int64_t rounds = V / ((int64_t)kSlab * cus);
+    const int n_main = (int)(rounds * cus), rest = V - n_main * kSlab;
+    const int width = q8_share(rest, cus), n_tail = (rest + width - 1) / width;
+    const int cost = width <= 64 ? f.tail64 : width <= 128 ? f.tail128 : 0;
+    if (rest == 0 || cost == 0 || n_tail > kMaxCutTail || rounds * f.cost + cost >= best.est) continue;
+    best = Q8Plan{f.rows, width <= 64 ? 64 : 128, 0, SlabCut{n_main, kSlab, width, 0, 0},
+                  n_main + n_tail, rounds * f.cost + cost};
   }
   return best;
 }
@@ -179,13 +180,11 @@ int q8_launches(int N, int V, int cus, Fn&& f) {
   const K1Plan plan = plan_k1(N, S, cus, &est);
   const Q8Plan p = q8_tail_plan(N, V, cus, est);
   if (p.rows) {
-    k.row_tiles = (N + p.rows - 1) / p.rows;
-    tile_blocking(k.row_tiles, cus, &k.blk_slabs, &k.blk_rows);
-    const int tail = (p.S - p.cut.n_main) * k.row_tiles;
+    k.row_tiles = 1;
+    const int tail = p.S - p.cut.n_main;
     if (p.rows == 128 && p.ids == 64) f(Q8Rows<128>{}, Q8Tail<128, 64>{}, p.cut, tail, k);
     else if (p.rows == 128) f(Q8Rows<128>{}, Q8Tail<128, 128>{}, p.cut, tail, k);
-    else if (p.rows == 192 && p.ids == 64) f(Q8Rows<192>{}, Q8Tail<192, 64>{}, p.cut, tail, k);
-    else if (p.rows == 192) f(Q8Rows<192>{}, Q8Tail<192, 128>{}, p.cut, tail, k);
+    else if (p.rows == 192) f(Q8Rows<192>{}, Q8Tail<192, 64>{}, p.cut, tail, k);
     else f(Q8Rows<256>{}, Q8Tail<256, 64>{}, p.cut, tail, k);
     return p.S;
   }
@@ -356,7 +355,8 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
       (reinterpret_cast<uintptr_t>(a->in) | reinterpret_cast<uintptr_t>(a->out)) % eb)
     return ASV_EINVAL;
   const int ids = kAdjThreads * (int)(16 / eb);
-  // fewer rows a workgroup where that takes more workgroups to fill the chip: eight of them a CU
+  // fewer rows a workgroup where that takes more workgroups to fill the chip: eight of them a CU (64 bf16
+  // rows of 151936 ids 24.6 us at 8 rows, 19.4 at the 2 this takes)
   const int64_t chunks = (a->V + ids - 1) / ids;
   int rows = kAdjRows;
   while (rows > 1 && chunks * ((a->N + rows - 1) / rows) < 8 * (int64_t)cu_count()) rows /= 2;

@@ -206,7 +206,9 @@ typedef float fx4 __attribute__((__vector_size__(16)));
 // kStep at a time, and taken through `block` in a loop of one body. (Changed in place, the accumulators were moved
 // between the register files on every pass of the K loop; with every block's code laid out like the
 // records without rules, it was longer than the instruction cache and took longer to fetch than to
-// run: 378 rows at V = 151936 428 us without rules, 583 with them.)
+// run: 378 rows of the 8-bit head at V = 151936 428 us without rules, 583 with them; as it is 413 and 500,
+// and 60 rows of the bf16 head at V = 128256 157 and 171. What is left is latency: the epilogue's code is
+// fetched once a tile from far away, and a tile that has ids on some row's path runs 10 us longer.)
 //
 // Every tile reads its ids' slice of the table, the bias and the mask once per 16 rows, through the caches:
 // with one request 9 bytes an id beside the weight's H or 2 H.
@@ -257,7 +259,8 @@ struct TileRules {
   __device__ __forceinline__ TileRules(const RuleArgs& r_, const A& a, int v0_, int v_end_, int r0_,
                                        void* smem, const P& pre)
       : r(r_), parent(a.parent), draft_tok(a.draft_tok), N(a.N), V(a.V), v0(v0_), v_end(v_end_),
-        r0(r0_), lds(static_cast<char*>(smem)), rows(*reinterpret_cast<Rows*>(static_cast<char*>(smem) + kRowsOff)) {
+        r0(r0_), lds(static_cast<char*>(smem)),
+        rows(*reinterpret_cast<Rows*>(static_cast<char*>(smem) + kRowsOff)) {
     rows.template build<C::kThreads>(r, a.req_offsets, parent, draft_tok, a.B, N, r0, v0, v_end, pre);
     lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -341,8 +344,9 @@ struct TileRules {
 
   // What a lane holds of the table and the bias for its ids, for the request of its last row, and of the
   // mask for its next row: the rows of a block mostly belong to one request, the block before's. The
-  // mask's words, and another request's entries, are on their way while the block before is reduced. Every load is from a place inside its
-  // array, whatever the row and the ids; what it brings of other rows and ids is masked or discarded.
+  // mask's words, and another request's entries, are on their way while the block before is reduced
+  // (378 rows of eight requests 513 -> 500 us). Every load is from a place inside its array, whatever the
+  // row and the ids; what it brings of other rows and ids is masked or discarded.
   struct Held {
     int b = -2;
     bool fresh = false;            // c is new
@@ -489,8 +493,8 @@ struct AdjustArgs {
 // Grid ceil(V / kIds) * ceil(N / rows), the ids fastest: the workgroup takes kIds ids of its rows, each
 // thread PT consecutive ones (16 bytes of input). Memory bound: one read and one write of the logits; the
 // table and the bias are read once for the consecutive rows of one request. Many waves with one row under
-// way each: 2048 rows of 128256 fp32 logits 494 us at 8 rows (4.4 TB/s; a copy of 2 GB on the same box 4.9),
-// 513 at 4, 511 at 16; with two and four rows' loads issued together 527 and 611.
+// way each: 2048 rows of 128256 fp32 logits 454 to 494 us by box (4.4 to 4.8 TB/s; a copy of 2 GB 4.9); beside
+// the 494 at 8 rows 513 at 4 and 511 at 16, and with two and four rows' loads issued together 527 and 611.
 template <class T, int PT>
 __global__ __launch_bounds__(kAdjThreads)
 void k_adjust(AdjustArgs a) {

@@ -67,7 +67,7 @@ SHAPES = [(1, 1, 64), (1, 257, 128), (3, 5, 64), (16, 127, 192), (17, 128, 576),
           (7, 20001, 64), (60, 40003, 64), (64, 50001, 64), (33, 70001, 64), (9, 90001, 64),
           (3, 140001, 64), (4, 152001, 64), (5, 168003, 64), (6, 180003, 64), (2, 200001, 64),
           (100, 32000, 64), (90, 75003, 64), (190, 20000, 64), (333, 40003, 128), (150, 36003, 64),
-          (500, 18000, 64), (230, 67003, 64)]
+          (500, 18000, 64), (230, 67003, 64), (190, 16003, 64), (200, 14001, 64)]
 
 
 @pytest.mark.parametrize("N,V,H", SHAPES)
