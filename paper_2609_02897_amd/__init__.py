@@ -190,7 +190,7 @@ def _same_device(device, **tensors):
 class PackedLmHead(NamedTuple):
     """An LM-head weight in a packed tile layout: ``kind`` "target" (``asv_pack_lm_head``,
     [256 rows][64 columns] tiles, for ``verify``), "draft" (``asv_pack_draft_head``, [64][64]
-    tiles, for ``draft_step``) or "fp8" (e4m3 codes in [256][128] tiles and the scales of their
+    tiles, for ``draft_step``) or "fp8" (e4m3 codes in [256][64] tiles and the scales of the
     128 x 128 blocks, for ``verify`` and ``lm_head_logits``). Tiles are stored column block major,
     zero rows past V."""
     data: "torch.Tensor"             # flat: bf16, packed_*_bytes(V, H) / 2 values; "fp8": uint8

@@ -330,6 +330,54 @@ def test_malformed_offsets_on_the_8_bit_head(asv, dev, offsets):
         assert torch.equal(a.accepted_len, b.accepted_len) and torch.equal(a.bonus_token, b.bonus_token)
 
 
+CUTS = [([60], 20000), ([60], 40003), ([5, 44], 70001), ([64], 100001), ([33], 128256), ([60], 152001),
+        ([7, 50], 168003), ([61], 181003), ([20], 200001), ([30, 40, 30], 20000), ([100], 32000),
+        ([70, 58], 75003), ([190], 16003), ([90, 100], 67003), ([100, 101, 55], 14001), ([256], 70003),
+        ([80, 70, 90, 93], 40003), ([150, 150], 36003), ([500], 18000), ([378], 151936), ([300, 301], 70003)]
+
+
+@pytest.mark.parametrize("sizes,V", CUTS)
+def test_rules_over_every_cut(asv, dev, sizes, V):
+    """Weights and hidden states whose products and sums fp32 and both heads hold exactly: verification with
+    rules on the bf16 and on the 8-bit head gives the ruled logits' own maxima, argmaxes and drafted logits,
+    bit for bit, over every tile family and cut of the ids."""
+    import torch
+    H, B = 64, len(sizes)
+    rng = np.random.default_rng([V, B])
+    g = torch.Generator(device=dev).manual_seed(V)
+    def exact(*s):                                        # +-1/2, 1, 2 or 4
+        return ((2.0 ** torch.randint(-1, 3, s, device=dev, generator=g)) *
+                (2 * torch.randint(0, 2, s, device=dev, generator=g) - 1)).bfloat16()
+    parent, off = _trees(rng, sizes)
+    N = int(off[-1])
+    x, w = exact(N, H), exact(V, H)
+    parent, off = _t(parent, dev), _t(off, dev)
+    tok = torch.randint(0, V, (N,), device=dev, generator=g, dtype=torch.int32)
+    tok[N // 3::4] = tok[0]                               # ids that many paths share
+    ids = torch.randint(0, V, (B, 500), device=dev, generator=g, dtype=torch.int32)
+    counts, _ = asv.token_counts(ids.view(-1), 500 * torch.arange(B + 1, dtype=torch.int32, device=dev), V)
+    rules = asv.LogitRules(counts, 1.0 + torch.rand(B, device=dev, generator=g),
+                           torch.rand(B, device=dev, generator=g), torch.rand(B, device=dev, generator=g),
+                           torch.randn((B, V), device=dev, generator=g),
+                           torch.randint(-2 ** 31, 2 ** 31, (N, -(-V // 32)), device=dev, generator=g,
+                                         dtype=torch.int64).int())
+    head = asv.quantize_lm_head(w)
+    zr = asv.adjust_logits(asv.lm_head_logits(x, head), rules, off, parent, tok)
+    top = zr.max(1).values
+    arg = (zr == top[:, None]).int().argmax(1).int()
+    kid = parent >= 0
+    drafted = zr[parent.long().clamp(min=0), tok.long()][kid]
+    lse = torch.logsumexp(zr.double(), 1)
+    tau = torch.full((B,), 0.3, device=dev)
+    for weight in (head, w, asv.pack_lm_head(w)):
+        out = asv.verify(x, weight, tok, parent, off, tau, rules=rules)
+        torch.cuda.synchronize()
+        assert not out.req_status.any()
+        assert torch.equal(out.row_max, top) and torch.equal(out.row_argmax, arg)
+        assert torch.equal(out.drafted_logit[kid], drafted)
+        assert bool(((out.row_lse.double() - lse).abs() < 1e-4).all())
+
+
 def test_refusals_of_the_binding(asv, dev):
     import torch
     V, H, N = 300, 64, 4
