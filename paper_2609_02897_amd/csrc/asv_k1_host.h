@@ -46,12 +46,13 @@ struct K1Plan {
   int n1;          // == S: one launch of tile a
 };
 
-// est: the plan's estimate (beyond 64 rows).
-K1Plan plan_k1(int N, int S, int cus, int64_t* est_out = nullptr) {
+// est: the plan's estimate (beyond 64 rows). cost: of a round of 128-, 192- and 256-row tiles.
+constexpr int kK1Cost[3] = {62, 80, 98};
+K1Plan plan_k1(int N, int S, int cus, int64_t* est_out = nullptr, const int* cost = kK1Cost) {
   if (N <= 64) return K1Plan{Tile::kRows64, Tile::kRows64, S};
   struct Family { Tile tile; int rows; int cost; };
-  const Family families[3] = {{Tile::kRows128, 128, 62}, {Tile::kRows192, 192, 80},
-                              {Tile::kRows256, 256, 98}};
+  const Family families[3] = {{Tile::kRows128, 128, cost[0]}, {Tile::kRows192, 192, cost[1]},
+                              {Tile::kRows256, 256, cost[2]}};
   auto rounds = [&](int64_t tiles) { return (tiles + cus - 1) / cus; };
   K1Plan best{Tile::kRows128, Tile::kRows128, S};
   int64_t best_est = INT64_MAX;

@@ -135,35 +135,44 @@ Q8Plan q8_rows64(int V, int cus) {
   return tailed(256, a_cu, width <= 128 ? width : q8_share(rest, 2 * c));
 }
 
+// us of a round of 128-, 192- and 256-row tiles at H = 4096, with records and with the logits stored, where
+// the 256-row tile's accumulators fill the registers and it stores as it goes: 2048 rows at V = 128256
+// 1714, 1657 and 1550 with records, 1744, 1685 and 1837 with logits; 640 rows 547, 604 and 572, and 558,
+// 606 and 686. (K1's rounds of bf16 take 62, 80 and 98.)
+constexpr int kQ8Records[3] = {56, 77, 98}, kQ8Logits[3] = {56, 78, 117};
+
 // Up to 256 rows, in one row tile: whole rounds of 256-id tiles and a tail of one narrower tile a CU, where
-// that is estimated to be faster than the best plan over whole slabs (by K1's costs: its rounds are in the
-// same proportion here, 64, 77 and 97 us). us of bf16 logits at H = 4096 on weights that are not in the caches,
-// whole slabs -> with the tail: 100 rows, V = 16000 55 -> 40, 32000 58 -> 55, 70003 119 -> 101; 128 rows,
-// 32000 56 -> 49, 75003 127 -> 110, 90003 129 -> 125; 190 rows, 16000 56 -> 49, 67003 148 -> 140; 256 rows,
-// 14000 56 -> 48, 70003 195 -> 192. Tails of 128 ids lose at 190 rows (20000: 56 -> 65), and any behind two
-// row tiles (333 rows, 40003: 124 -> 137; 480 rows level).
-Q8Plan q8_tail_plan(int N, int V, int cus, int64_t plan_est) {
-  struct Family { int rows, cost, tail64, tail128; };
-  const Family families[3] = {{128, 62, 46, 57}, {192, 80, 60, 0}, {256, 98, 80, 0}};
+// that is estimated to be faster than the best plan over whole slabs. us of bf16 logits at H = 4096 on weights
+// that are not in the caches, whole slabs -> with the tail: 100 rows, V = 16000 55 -> 40, 32000 58 -> 55,
+// 70003 119 -> 101; 128 rows, 32000 56 -> 49, 75003 127 -> 110, 90003 129 -> 125; 190 rows, 16000 56 -> 49,
+// 67003 148 -> 140; 256 rows, 14000 56 -> 48; 250 rows with records, 75003 173 -> 163. Tails of 128 ids
+// lose at 190 rows (20000: 56 -> 65), and any behind two row tiles (333 rows, 40003: 124 -> 137; 480 rows
+// level).
+Q8Plan q8_tail_plan(int N, int V, int cus, const int* cost, int64_t plan_est) {
+  // a tail of 64 and of 128 ids (0: not taken), and what it takes more behind whole rounds
+  struct Family { int rows, tail64, tail128, behind; };
+  const Family families[3] = {{128, 40, 50, 3}, {192, 49, 0, 11}, {256, 48, 0, 20}};
   Q8Plan best{};
   best.est = plan_est;
-  for (const Family& f : families) {
+  for (int i = 0; i < 3; ++i) {
+    const Family& f = families[i];
     if (N > f.rows) continue;
     const int64_t rounds = V / ((int64_t)kSlab * cus);
     const int n_main = (int)(rounds * cus), rest = V - n_main * kSlab;
     const int width = q8_share(rest, cus), n_tail = (rest + width - 1) / width;
-    const int cost = width <= 64 ? f.tail64 : width <= 128 ? f.tail128 : 0;
-    if (rest == 0 || cost == 0 || n_tail > kMaxCutTail || rounds * f.cost + cost >= best.est) continue;
+    const int tail = width <= 64 ? f.tail64 : width <= 128 ? f.tail128 : 0;
+    const int64_t est = rounds * cost[i] + tail + (rounds > 0 ? f.behind : 0);
+    if (rest == 0 || tail == 0 || n_tail > kMaxCutTail || est >= best.est) continue;
     best = Q8Plan{f.rows, width <= 64 ? 64 : 128, 0, SlabCut{n_main, kSlab, width, 0, 0},
-                  n_main + n_tail, rounds * f.cost + cost};
+                  n_main + n_tail, est};
   }
   return best;
 }
 
 // f(main family, tail family, cut, tiles of the tail, launch) for the launches of N rows; returns the
-// records a row writes.
+// records a row writes. cost: see kQ8Records.
 template <class Fn>
-int q8_launches(int N, int V, int cus, Fn&& f) {
+int q8_launches(int N, int V, int cus, const int* cost, Fn&& f) {
   asv_k1_launch k{};
   if (N <= 64) {
     const Q8Plan p = q8_rows64(V, cus);
@@ -177,8 +186,8 @@ int q8_launches(int N, int V, int cus, Fn&& f) {
   }
   const int S = (V + kSlab - 1) / kSlab;
   int64_t est = 0;
-  const K1Plan plan = plan_k1(N, S, cus, &est);
-  const Q8Plan p = q8_tail_plan(N, V, cus, est);
+  const K1Plan plan = plan_k1(N, S, cus, &est, cost);
+  const Q8Plan p = q8_tail_plan(N, V, cus, cost, est);
   if (p.rows) {
     k.row_tiles = 1;
     const int tail = p.S - p.cut.n_main;
@@ -204,7 +213,7 @@ int q8_launches(int N, int V, int cus, Fn&& f) {
 
 // What the launches of N rows will write a row.
 int q8_records(int N, int V, int cus) {
-  return q8_launches(N, V, cus, [](auto, auto, const SlabCut&, int, const asv_k1_launch&) {});
+  return q8_launches(N, V, cus, kQ8Records, [](auto, auto, const SlabCut&, int, const asv_k1_launch&) {});
 }
 
 template <class E>
@@ -215,7 +224,7 @@ int verify_fp8(const asv_verify_args* a, char* ws, hipStream_t s, const E& e) {
   LmheadArgs g = lmhead_args(a, L, ws, S);
   if (int rc = round_rows(a->hidden, a->w_lm, a->N, a->H, a->V, ws + L.bytes, s, &g)) return rc;
   if (int rc = draft_conf(a, L, ws, a->N <= 64 ? S : 0, s, &g.conf)) return rc;
-  q8_launches(a->N, a->V, cus,
+  q8_launches(a->N, a->V, cus, kQ8Records,
               [&](auto m, auto t, const SlabCut& cut, int n_tail, const asv_k1_launch& k) {
                 launch_lmhead<decltype(m), decltype(t)>(g, cut, n_tail, k, s,
                                                         K1Events{nullptr, nullptr}, e);
@@ -298,7 +307,7 @@ extern "C" int asv_lm_head_logits(const asv_logits_args* a, void* workspace,
   if (int rc = round_rows(a->hidden, a->w, a->N, a->H, a->V, static_cast<char*>(workspace), s, &g))
     return rc;
   const StoreArgs st{a->out, a->out_pitch, a->out_type};
-  q8_launches(a->N, a->V, cu_count(),
+  q8_launches(a->N, a->V, cu_count(), kQ8Logits,
               [&](auto m, auto t, const SlabCut& cut, int n_tail, const asv_k1_launch& k) {
                 using M = decltype(m);
                 k_lmhead_logits<M, decltype(t)>
