@@ -412,7 +412,7 @@ def run(s):
     if s["op"] == "logits":
         return asv.lm_head_logits(s["hidden"], s["head"], dtype=s["dtype"])
     if s["op"] == "counts":
-        return asv.token_counts(s["tok"], s["off"], s["V"], s["prompt"])[0].long()
+        return asv.token_counts(s["tok"], s["off"], s["V"], s["prompt"])[0]
     rules = None if s["rules"] is None else asv.LogitRules(**s["rules"])
     if s["op"] == "adjust":
         return asv.adjust_logits(s["logits"], rules, s["off"], s["parent"], s["tok"], out=s["out"])
