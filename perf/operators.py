@@ -408,6 +408,9 @@ def _plain(s):
 def run(s):
     if not own:
         return _plain(s)
+    elif s["op"] == "counts" and "int32" not in s:
+        # the call's table is int32; the plain form gives the same counts as int64
+        return run({**s, "int32": True}).long()
     import paper_2609_02897_amd as asv
     if s["op"] == "logits":
         return asv.lm_head_logits(s["hidden"], s["head"], dtype=s["dtype"])
