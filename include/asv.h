@@ -394,7 +394,8 @@ typedef struct asv_logit_rules {
  * ASV_W_FP8, w_lm is the packed copy above (16-byte aligned). Every output is that of the ruled logits.
  * With rules, a drafted token whose ruled logit is -inf is never accepted (at tau = 0 neither), and a row that
  * they leave nothing has row_max = row_lse = -inf and row_argmax = -1, which is the bonus token of a
- * walk that ends there. rules: NULL or all NULL for none. Workspace:
+ * walk that ends there. A row with ids of +inf (a bias that forces them, a repetition of 0) has row_max =
+ * row_lse = +inf, and each of these ids is accepted where it is drafted. rules: NULL or all NULL for none. Workspace:
  * asv_verify_ruled_workspace_bytes of the same layout; never falls as B, N or V grow. Results and
  * errors otherwise as asv_verify's; ASV_EINVAL also for a bad bias_pitch, misaligned rules, or rules on
  * more than 65535 rows. */

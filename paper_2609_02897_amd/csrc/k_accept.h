@@ -278,12 +278,22 @@ __device__ __forceinline__ void finish_request(const AcceptArgs& a, int b, int n
 }
 
 // Eq. (1) for a node with drafted logit g under a row of maximum mx. Under sampling rules (RULED) a
-// token that they rule out (a logit of -inf) is never accepted, not even at kappa = 0.
+// token that they rule out (a logit of -inf) is never accepted, not even at kappa = 0, and one that
+// they force (+inf, as the row's maximum then is) always is, though inf - inf is no number.
 template <bool RULED>
 __device__ __forceinline__ bool node_ok(bool top1, float kappa, float g, float mx, float ln_kappa) {
   const bool ok = top1 || kappa == 0.f || g - mx >= ln_kappa;
-  if constexpr (RULED) return ok && g != kNegInf;
+  if constexpr (RULED) return (ok || g == mx) && g != kNegInf;
   else return ok;
+}
+
+// The log-sum-exp of a row's merged record. Under sampling rules +inf where they force an id: the
+// record's sum is no number there, as every exponent is inf - inf or -inf.
+template <bool RULED>
+__device__ __forceinline__ float row_lse_of(const Rec& r) {
+  const float lse = r.m + __builtin_amdgcn_logf(r.s) * 0.69314718055994531f;
+  if constexpr (RULED) return r.m == -kNegInf ? r.m : lse;
+  else return lse;
 }
 
 // The argmax of a row: under sampling rules -1 where they leave the row nothing.
@@ -523,7 +533,7 @@ void k_merge_accept(int S, const float* __restrict__ rec_m, const float* __restr
     const Rec r = merge_row_rest(first, rbase, S, lane, rec_m, rec_s, rec_a);
     if (lane == 0) {
       st_device(row_max + n, r.m);
-      row_lse[n] = r.m + __builtin_amdgcn_logf(r.s) * 0.69314718055994531f;
+      row_lse[n] = row_lse_of<RULED>(r);
       st_device(row_argmax + n, row_arg_of<RULED>(r.a));
     }
   }
@@ -599,7 +609,7 @@ void k_slab_merge(int N, int S, const float* __restrict__ rec_m, const float* __
   const Rec r = merge_row_rest(first, base, S, lane, rec_m, rec_s, rec_a);
   if (lane == 0) {
     row_max[n] = r.m;
-    row_lse[n] = r.m + __builtin_amdgcn_logf(r.s) * 0.69314718055994531f;
+    row_lse[n] = row_lse_of<RULED>(r);
     row_argmax[n] = row_arg_of<RULED>(r.a);
   }
 }
