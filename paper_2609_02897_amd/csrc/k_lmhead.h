@@ -952,7 +952,13 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
     m = max_raw(__uint_as_float(lo), __uint_as_float(hi));
     lane_halves<32>(__float_as_uint(m), lo, hi);
     m = max_raw(__uint_as_float(lo), __uint_as_float(hi));
-    const float mb = m * kLog2e;
+    // Exponents z log2(e) - m log2(e): the second product is rounded, by up to 2^-24 of itself, which for a
+    // maximum past 2^31 is more than a float's exponent range (rules with a bias of -1e10 on a whole slab left
+    // its row no log-sum-exp). From 2^29 on other logits are 32 below the maximum at least and count
+    // for nothing, so any scale does: 1, under which the difference is exact.
+    float scale = kLog2e;
+    if constexpr (E::kRules) scale = fabsf(m) < 536870912.f ? kLog2e : 1.f;
+    const float mb = m * scale;
     float sum = 0.f;
     int kbest = -1;
     // groups of four, comparisons, exponentials, selects and adds apart: left to itself the compiler
@@ -964,7 +970,7 @@ __device__ __forceinline__ void lmhead_block(const LmheadArgs& a, int v0, int v_
 #pragma unroll
       for (int q = 3; q >= 0; --q) {
         const float z = entry(g + q);
-        t[q] = fmaf(z, kLog2e, -mb);
+        t[q] = fmaf(z, scale, -mb);
         best[q] = __builtin_amdgcn_ballot_w64(z == m);
       }
       __builtin_amdgcn_sched_barrier(0);

@@ -123,3 +123,26 @@ def test_infinite_ruled_logits(asv, dev, head, B, n, V):
     rep = np.ones(B, np.float32)
     rep[::2] = 0.0
     s.check(asv, head, dict(counts=counts, repetition=rep))
+
+
+@pytest.mark.parametrize("B,n,V", STEPS)
+@pytest.mark.parametrize("head", HEADS)
+@pytest.mark.parametrize("size", [1e6, 1e9, 1e10, 1e30, FMAX])
+def test_huge_finite_biases(asv, dev, head, size, B, n, V):
+    """Ids banned and forced by a bias that is finite: bans of every id of whole slabs, of all ids of a row but one
+    and of all of them, and forced ids that leave every other logit behind."""
+    s = Step(dev, B, n, V, 2)
+    v = np.arange(V)
+    bias = np.zeros((B, V), np.float32)
+    bias[0] = np.where(v // 64 % 2 == 0, -size, 0)
+    bias[1] = np.where(v == V - 2, 0, -size)
+    if B > 2:
+        bias[2] = -size
+        bias[3, s.rng.random(V) < 0.4] = size
+        bias[3, s.rng.random(V) < 0.4] = -size
+    if B > 4:
+        bias[4, V // 3] = size
+    # as many requests as there are, with these rules in turn
+    for b in range(5, B):
+        bias[b] = bias[b % 5]
+    s.check(asv, head, dict(bias=bias))
