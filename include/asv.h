@@ -410,7 +410,9 @@ typedef struct asv_adjust_args {
                                      req_offsets N == B */
   int32_t type;                   /* ASV_F32, ASV_BF16 or ASV_F16, of in and out */
   const void *in;                 /* [N] rows of V logits, in_pitch elements apart */
-  void *out;                      /* the same, out_pitch apart; may be `in` with the same pitch. Elements
+  void *out;                      /* the same, out_pitch apart; may be `in` with the same pitch. Else no
+                                     element of it is one of `in`; its rows may lie between those
+                                     of `in` where both have one pitch. Elements
                                      V .. out_pitch - 1 of a row are left as they were */
   int64_t in_pitch, out_pitch;    /* >= V */
   const int32_t *req_offsets;     /* [B+1] as in asv_verify, or NULL: row n is request n */

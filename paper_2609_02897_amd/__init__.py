@@ -492,7 +492,8 @@ def adjust_logits(logits, rules: LogitRules, req_offsets=None, parent=None, draf
     bfloat16 or float16 [N, V], rows any stride >= V apart. Row n belongs to the request of
     req_offsets int32 [B+1], or to request n without it; with a tree's parent and draft_tok int32 [N],
     a row also counts the tokens drafted on its path. ``out``: a matrix of the same type and shape, may be ``logits``
-    itself; a new one by default."""
+    itself, else shares no element with it (its rows may lie between those of ``logits`` where both have the same
+    stride); a new one by default."""
     import torch
     N, V = logits.shape
     B = N if req_offsets is None else req_offsets.shape[0] - 1

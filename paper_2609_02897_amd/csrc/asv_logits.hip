@@ -30,6 +30,18 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
   return x < y + nb && y < x + na;
 }
 
+// Whether matrices of N rows of V elements of `eb` bytes, aligned to their elements, share one. Rows of one
+// pitch may lie between each other's; with two pitches the ranges from the first to the last element count.
+bool rows_overlap(const void* a, int64_t pitch_a, const void* b, int64_t pitch_b, int N, int V,
+                  size_t eb) {
+  const uint64_t last = (uint64_t)(N - 1);
+  if (!overlap(a, (last * pitch_a + V) * eb, b, (last * pitch_b + V) * eb)) return false;
+  if (pitch_a != pitch_b) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const uint64_t between = (x < y ? y - x : x - y) / eb % (uint64_t)pitch_a;
+  return between < (uint64_t)V || (uint64_t)pitch_a - between < (uint64_t)V;
+}
+
 template <bool QUANT>
 int pack_fp8(const void* w, const uint8_t* scale, int V, int H, void* packed, uint64_t bytes,
              void* stream) {
@@ -371,10 +383,9 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
   while (rows > 1 && chunks * ((a->N + rows - 1) / rows) < 8 * (int64_t)cu_count()) rows /= 2;
   const int64_t grid = chunks * ((a->N + rows - 1) / rows);
   if (grid > INT32_MAX) return ASV_EINVAL;
-  // out is in, or apart from it
-  if (a->in == a->out ? a->in_pitch != a->out_pitch
-                      : overlap(a->in, ((uint64_t)(a->N - 1) * a->in_pitch + a->V) * eb, a->out,
-                                ((uint64_t)(a->N - 1) * a->out_pitch + a->V) * eb))
+  // out is in (one row has no pitch), or apart from it
+  if (a->in == a->out ? a->in_pitch != a->out_pitch && a->N > 1
+                      : rows_overlap(a->in, a->in_pitch, a->out, a->out_pitch, a->N, a->V, eb))
     return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();
