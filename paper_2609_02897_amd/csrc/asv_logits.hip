@@ -67,7 +67,9 @@ size_t rounded_bytes(int N, int H) { return align_up((size_t)N * H * 2); }
 int round_rows(const uint16_t* hidden, const void* w, int N, int H, int V, char* to, hipStream_t s,
                LmheadArgs* g) {
   uint16_t* x = reinterpret_cast<uint16_t*>(to);
-  k_round_rows<<<dim3(N, (H + kRoundCols - 1) / kRoundCols), kRoundThreads, 0, s>>>(hidden, H, x);
+  for (int n = 0; n < N; n += kRoundRows)
+    k_round_rows<<<dim3(std::min(N - n, kRoundRows), (H + kRoundCols - 1) / kRoundCols), kRoundThreads, 0,
+                   s>>>(hidden + (size_t)n * H, H, x + (size_t)n * H);
   g->X = x;
   g->W = static_cast<const uint16_t*>(w);
   g->H = H;

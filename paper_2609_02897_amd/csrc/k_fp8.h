@@ -76,8 +76,11 @@ __device__ __forceinline__ int max_abs_bf16(const uint4& x) {
 constexpr int kRoundThreads = 256;
 constexpr int kRoundCols = kRoundThreads * 8;
 
-// K12. Grid (N, ceil(H / kRoundCols)): eight columns a thread, a block per 16 lanes. X bf16 [N][H], out the
-// values that its codes and scales stand for, bf16 [N][H].
+// K12. Grid (rows, ceil(H / kRoundCols)): eight columns a thread, a block per 16 lanes. X bf16 [N][H] from the
+// launch's first row on, out the values that its codes and scales stand for, bf16 [N][H]. A launch has fewer
+// than 2^32 threads along x, so at most kRoundRows rows.
+constexpr int kRoundRows = 1 << 23;
+
 static __global__ __launch_bounds__(kRoundThreads)
 void k_round_rows(const uint16_t* __restrict__ X, int H, uint16_t* __restrict__ out) {
   const int col = blockIdx.y * kRoundCols + threadIdx.x * 8;
