@@ -406,8 +406,9 @@ int asv_verify_ruled(const asv_verify_args *args, const asv_logit_rules *rules, 
 
 /* Arguments of asv_adjust_logits: the rules on logits in memory. */
 typedef struct asv_adjust_args {
-  int32_t B, N, V;                /* host ints: B >= 0, N >= B, V > 0, N and V < 2^30; without
-                                     req_offsets N == B */
+  int32_t B, N, V;                /* host ints: B >= 0, N >= B, V > 0, N and V < 2^30,
+                                     ceil(N / 8) * ceil(V / 1024) < 2^24 (16-bit types: V / 2048);
+                                     without req_offsets N == B */
   int32_t type;                   /* ASV_F32, ASV_BF16 or ASV_F16, of in and out */
   const void *in;                 /* [N] rows of V logits, in_pitch elements apart */
   void *out;                      /* the same, out_pitch apart; may be `in` with the same pitch. Else no
@@ -428,7 +429,8 @@ int asv_adjust_logits(const asv_adjust_args *args, void *stream);
 
 /* Arguments of asv_token_counts. */
 typedef struct asv_counts_args {
-  int32_t B, T, V;                /* host ints: B >= 0, T >= 0, 0 < V < 2^30 */
+  int32_t B, T, V;                /* host ints: B >= 0, T >= 0, 0 < V < 2^30,
+                                     B * ceil(V / 20480) < 2^22 */
   int32_t add;                    /* 0: write the table; 1: add to it (asv_commit's tokens, say) */
   const int32_t *tok;             /* [T] token ids */
   const int32_t *tok_offsets;     /* [B+1]: request b's tokens are tok[tok_offsets[b]] .. up to

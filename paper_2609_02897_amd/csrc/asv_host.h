@@ -19,6 +19,11 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A launch along x holds fewer than 2^32 threads; beyond, workgroups are dropped without an error.
+inline bool launch_fits(int64_t workgroups, int threads) {
+  return workgroups >= 0 && workgroups * threads < (int64_t)1 << 32;
+}
+
 // Compute units of the current device, queried once per device.
 int cu_count();
 

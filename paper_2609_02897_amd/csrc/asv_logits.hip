@@ -384,7 +384,7 @@ extern "C" int asv_adjust_logits(const asv_adjust_args* a, void* stream) {
   int rows = kAdjRows;
   while (rows > 1 && chunks * ((a->N + rows - 1) / rows) < 8 * (int64_t)cu_count()) rows /= 2;
   const int64_t grid = chunks * ((a->N + rows - 1) / rows);
-  if (grid > INT32_MAX) return ASV_EINVAL;
+  if (!launch_fits(grid, kAdjThreads)) return ASV_EINVAL;
   // out is in (one row has no pitch), or apart from it
   if (a->in == a->out ? a->in_pitch != a->out_pitch && a->N > 1
                       : rows_overlap(a->in, a->in_pitch, a->out, a->out_pitch, a->N, a->V, eb))
@@ -411,8 +411,8 @@ extern "C" int asv_token_counts(const asv_counts_args* a, void* stream) {
   const int64_t share = ((int64_t)a->V + want - 1) / want;
   const int ids = (int)std::min<int64_t>(kCountIds, std::max<int64_t>(kCountLeast, (share + 3) / 4 * 4));
   const int64_t grid = ((int64_t)a->V + ids - 1) / ids * a->B;
-  if ((!a->tok && a->T > 0) || !a->tok_offsets || !a->counts || !a->req_status || grid > INT32_MAX ||
-      !aligned4(a->tok, a->tok_offsets, a->prompt_len, a->counts, a->req_status))
+  if ((!a->tok && a->T > 0) || !a->tok_offsets || !a->counts || !a->req_status ||
+      !launch_fits(grid, kCountThreads) || !aligned4(a->tok, a->tok_offsets, a->prompt_len, a->counts, a->req_status))
     return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   (void)hipGetLastError();
