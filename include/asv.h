@@ -108,7 +108,9 @@ typedef struct asv_verify_args {
   int32_t B, N, H, V;             /* host ints: B >= 0, N >= B (N == 0 iff B == 0),
                                      H > 0 with H % 64 == 0 and H <= 2^20, V > 0,
                                      N, V < 2^30 and ceil(V / 256) * ceil(N / 64) < 2^31
-                                     (the LM-head kernel's largest workgroup count) */
+                                     (the LM-head kernel's largest workgroup count). A step
+                                     whose launches would have 2^32 threads is refused:
+                                     N > 2^26 - 4, or 2^24 LM-head workgroups in one launch */
   const uint16_t *hidden;         /* [N][H] bf16 final hidden states, 16-byte aligned */
   const uint16_t *w_lm;           /* [V][H] bf16 LM-head weight, or its packed copy (see
                                      w_lm_layout), 16-byte aligned */

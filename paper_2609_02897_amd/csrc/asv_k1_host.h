@@ -584,6 +584,13 @@ bool workspace_ok(const void* workspace, uint64_t have, size_t need) {
   return workspace && have >= need && reinterpret_cast<uintptr_t>(workspace) % kAlign == 0;
 }
 
+// Every launch of a step fits a dispatch: an LM-head launch of at most lm_tiles workgroups, and those of
+// finish_verify.
+bool step_fits(const asv_verify_args* a, int64_t lm_tiles) {
+  return launch_fits(lm_tiles, kConfWaves * kWave) &&
+         launch_fits(((int64_t)a->N + 3) / 4, 4 * kWave) && launch_fits(a->B, kWave);
+}
+
 // The draft logits' records (K4). They only need the inputs: where `tiles` (the tiles of a launch of
 // K1 whose tiles can take a share each) are enough, they get the shares, which saves K4's launch
 // (8 rows at V = 128256, one request: 165.6 -> 162.9 us); else K4 is launched.
@@ -633,8 +640,10 @@ template <class E>
 int verify_bf16(const asv_verify_args* a, char* ws, const Tile* tile, hipEvent_t begin,
                 hipEvent_t end, hipStream_t s, const E& e) {
   const Layout L = layout(a->B, a->N, a->V);
-  (void)hipGetLastError();
   const K1Step step = k1_step(a->N, a->V, cu_count(), tile, !E::kRules);
+  for (int q = 0; q < step.n_plan; ++q)
+    if (!step_fits(a, (int64_t)step.plan[q].n_slabs * step.plan[q].row_tiles)) return ASV_EINVAL;
+  (void)hipGetLastError();
   const Cut64& cut64 = step.cut64;
   const CutWide& wide = step.wide;
   LmheadArgs g = lmhead_args(a, L, ws, step.S);

@@ -225,15 +225,16 @@ int q8_launches(int N, int V, int cus, const int* cost, Fn&& f) {
   return S;
 }
 
-// What the launches of N rows will write a row.
-int q8_records(int N, int V, int cus) {
-  return q8_launches(N, V, cus, kQ8Records, [](auto, auto, const SlabCut&, int, const asv_k1_launch&) {});
-}
-
 template <class E>
 int verify_fp8(const asv_verify_args* a, char* ws, hipStream_t s, const E& e) {
   const Layout L = layout(a->B, a->N, a->V, q8_max_records(a->N, a->V));
-  const int cus = cu_count(), S = q8_records(a->N, a->V, cus);
+  const int cus = cu_count();
+  int64_t tiles = 0;
+  const int S = q8_launches(a->N, a->V, cus, kQ8Records,
+                            [&](auto, auto, const SlabCut& cut, int n_tail, const asv_k1_launch& k) {
+                              tiles = std::max(tiles, (int64_t)cut.n_main * k.row_tiles + n_tail);
+                            });
+  if (!step_fits(a, tiles)) return ASV_EINVAL;
   (void)hipGetLastError();
   LmheadArgs g = lmhead_args(a, L, ws, S);
   if (int rc = round_rows(a->hidden, a->w_lm, a->N, a->H, a->V, ws + L.bytes, s, &g)) return rc;

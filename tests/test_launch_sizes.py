@@ -35,3 +35,30 @@ def test_counts(lib):
         a.B, a.T, a.V, a.add = B, 9, V, 0
         a.tok, a.tok_offsets, a.counts, a.req_status = BIG, 2 * BIG, 3 * BIG, 9 * BIG
         assert lib.asv_token_counts(ctypes.byref(a), None) == asv.ASV_EINVAL, (B, V)
+
+
+@pytest.mark.parametrize("layout", [0, 1, _abi.W_FP8])
+def test_verify(lib, layout):
+    def call(B, N, V, ruled):
+        a = _abi.AsvVerifyArgs()
+        a.B, a.N, a.H, a.V, a.w_lm_layout = B, N, 64, V, layout
+        for i, f in enumerate(("hidden", "w_lm", "draft_tok", "parent", "req_offsets", "tau", "row_max",
+                               "row_lse", "row_argmax", "drafted_logit", "accept", "accepted_len",
+                               "bonus_token", "accepted_path", "req_status")):
+            setattr(a, f, (i + 1) * BIG)
+        a.params = asv.make_params()
+        if ruled:
+            rules = _abi.AsvLogitRules()
+            rules.repetition = 90 * BIG
+            return lib.asv_verify_ruled(ctypes.byref(a), ctypes.byref(rules), 80 * BIG, 1 << 60, None)
+        if layout == _abi.W_FP8:
+            return lib.asv_verify_ruled(ctypes.byref(a), None, 80 * BIG, 1 << 60, None)
+        return lib.asv_verify(ctypes.byref(a), 80 * BIG, 1 << 60, None)
+
+    # rows of the finishing step; workgroups of the LM head (256 ids x 256 rows at most)
+    for B, N, V in ((1, (1 << 26) - 3, 5), (1 << 26, 1 << 26, 1), (3, 1 << 29, 256), (1, 1 << 20, 1 << 21)):
+        assert call(B, N, V, False) == asv.ASV_EINVAL, (B, N, V)
+    # with rules, whose rows are at most 65535
+    V = 3 << 23                            # 98304 slabs x 256 row tiles of 256 rows, two launches at most
+    if layout != _abi.W_FP8:
+        assert call(1, 65535, V, True) == asv.ASV_EINVAL
