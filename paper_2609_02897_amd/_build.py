@@ -10,7 +10,7 @@ ROOT = os.path.dirname(_HERE)
 SOURCES = [os.path.join(_HERE, "csrc", f) for f in ("asv_api.hip", "asv_logits.hip",
                                                                 "asv_rules.hip")]
 HEADERS = [os.path.join(ROOT, "include", "asv.h")] + [
-    os.path.join(_HERE, "csrc", f) for f in ("asv_host.h", "asv_k1_host.h", "k_common.h",
+    os.path.join(_HERE, "csrc", f) for f in ("asv_host.h", "asv_k1_host.h", "asv_q8_host.h", "k_common.h",
                                                "k_lmhead.h", "k_reduce.h", "k_accept.h",
                                                "k_draft.h", "k_tree.h", "k_rules.h", "k_fp8.h")]
 OUT = os.path.join(_HERE, "libasv.so")
