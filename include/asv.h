@@ -379,8 +379,10 @@ int asv_lm_head_logits(const asv_logits_args *args, void *workspace, uint64_t wo
  *   z2 = g > 0 ? z1 - (presence[b] + frequency[b] * g) : z1
  *   z3 = z2 + bias[b][v]
  *   z4 = bit v of allowed[n] set ? z3 : -inf
- * in fp32, whatever z3 is. Every pointer may be NULL: no history, 1, 0, 0, no bias, all allowed. The
- * values are applied as they are (a repetition of 0 divides by it). */
+ * in fp32, whatever z3 is, each operation rounded once, frequency * g not apart from its sum, and z / repetition
+ * taken as z * (1 / repetition), whose reciprocal is rounded and infinite below 2^-128. Every pointer may
+ * be NULL: no history, 1, 0, 0, no bias, all allowed. The values are applied as they are (a
+ * repetition of 0 divides by it: +inf). */
 typedef struct asv_logit_rules {
   const int32_t *counts;          /* [B][V] history table */
   const float *repetition;        /* [B] */

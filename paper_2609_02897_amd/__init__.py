@@ -375,8 +375,8 @@ def verify(hidden, w_lm, draft_tok, parent, req_offsets, tau, draft_logits=None,
 class LogitRules(NamedTuple):
     """Sampling rules of B requests with N rows on V ids (``asv_logit_rules``); None leaves one out.
     With g = how often an id was generated (``counts``) or drafted on the row's path and seen = g > 0
-    or in the prompt: the logit of a seen id is divided by ``repetition`` if positive, else
-    multiplied by it; an id with g > 0 loses presence + frequency * g; then the bias is added; ids
+    or in the prompt: the logit of a seen id is divided by ``repetition`` if positive (multiplied by its reciprocal, rounded
+    to float32), else multiplied by it; an id with g > 0 loses presence + frequency * g; then the bias is added; ids
     whose bit is not set get -inf."""
     counts: Optional["torch.Tensor"] = None       # i32 [B, V], from token_counts
     repetition: Optional["torch.Tensor"] = None   # f32 [B]
