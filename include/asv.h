@@ -215,7 +215,8 @@ typedef struct asv_draft_tree {
 typedef struct asv_draft_args {
   int32_t B, H, V;                /* host ints: B >= 0, H > 0 with H % 64 == 0,
                                      4 <= V < 2^30, 8 B H < 2^31, and the draft LM head's
-                                     workgroup count (slabs x row tiles) below 2^31 */
+                                     workgroup count (slabs x row tiles) below 2^31; a step is
+                                     refused from 2^24 of them on (2^23 beyond 64 rows) */
   int32_t step;                   /* host int: 0 (re)starts every tree from its shape */
   const uint16_t *hidden;         /* [4B][H] bf16 draft hidden states, 16-byte aligned */
   const uint16_t *w_draft;        /* [V][H] bf16 draft LM-head weight, 16-byte aligned */
@@ -269,7 +270,7 @@ int asv_draft_step(const asv_draft_args *args, void *workspace, uint64_t workspa
  * the root first (parent -1, draft_tok = root_tok[b], or -1 when root_tok is NULL), then the
  * kept pool nodes in pool order with global parent ids. An invalid tree gives n_b = 1.
  * tree: [B]; root_tok: [B] or NULL; parent, draft_tok: [n_cap]; req_offsets: [B+1] (always
- * written, also past n_cap); req_status: [B] ASV_DS_* bits. Returns ASV_EINVAL for B < 0,
+ * written, also past n_cap); req_status: [B] ASV_DS_* bits. Returns ASV_EINVAL for B < 0, B >= 2^24,
  * n_cap < 0 or null outputs, ASV_EHIP if a launch fails. */
 int asv_draft_prune(const asv_draft_tree *tree, int32_t B, const int32_t *root_tok,
                     int32_t n_cap, int32_t *parent, int32_t *draft_tok, int32_t *req_offsets,
@@ -284,7 +285,8 @@ int asv_draft_prune(const asv_draft_tree *tree, int32_t B, const int32_t *root_t
  * word k / 32 at position k % 32). pos or mask may be NULL to skip them. Requests whose
  * offsets or parents are malformed (ASV_RS_BAD_OFFSETS, ASV_RS_BAD_ROOT, ASV_RS_BAD_PARENT)
  * get neither; a request with more than 32 * mask_words nodes gets ASV_RS_MASK_SMALL and its
- * positions only. req_status: [B]. Returns ASV_EINVAL for bad sizes or null arguments. */
+ * positions only. req_status: [B]. Returns ASV_EINVAL for bad sizes (B >= 2^24 among them) or null
+ * arguments. */
 int asv_tree_meta(const int32_t *parent, const int32_t *req_offsets, int32_t B, int32_t N,
                   const int32_t *pos_base, int32_t mask_words, int32_t *pos, uint32_t *mask,
                   int32_t *req_status, void *stream);
@@ -311,7 +313,7 @@ typedef struct asv_commit_args {
 
 /* Commit one verification step. A request with ASV_RS_BAD_PATH commits only its root row and
  * bonus (length 0); entries that would land at index >= N are not written. Returns ASV_EINVAL
- * for bad sizes, null or misaligned pointers, ASV_EHIP if a launch fails. */
+ * for bad sizes (B >= 2^24 among them), null or misaligned pointers, ASV_EHIP if a launch fails. */
 int asv_commit(const asv_commit_args *args, void *stream);
 
 /* ---- Sampling rules and the 8-bit LM head. */

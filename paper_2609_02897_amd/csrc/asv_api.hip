@@ -413,6 +413,9 @@ extern "C" int asv_draft_step_tuned(const asv_draft_args* a, const asv_tuning* t
   const K1Events ev{reinterpret_cast<hipEvent_t>(tu.begin_event),
                     reinterpret_cast<hipEvent_t>(tu.end_event)};
   const DraftPlan p = plan_draft(a->B * kTopK, a->V, cu_count());
+  // four waves a workgroup up to 64 rows, eight beyond
+  if (!launch_fits((int64_t)p.cut.S * p.row_tiles, (a->B * kTopK <= 64 ? 4 : 8) * kWave))
+    return ASV_EINVAL;
   switch (p.tile) {
     case DraftTile::kRows32x64:
       launch_draft<TileFamily<64, 32, 2, 1, 4, 0, true, Mfma32>>(a, L, ws, p, s, ev);
@@ -484,7 +487,7 @@ extern "C" int asv_draft_step(const asv_draft_args* a, void* workspace, uint64_t
 extern "C" int asv_draft_prune(const asv_draft_tree* tree, int32_t B, const int32_t* root_tok,
                                int32_t n_cap, int32_t* parent, int32_t* draft_tok,
                                int32_t* req_offsets, int32_t* req_status, void* stream) {
-  if (B < 0 || n_cap < 0) return ASV_EINVAL;
+  if (B < 0 || n_cap < 0 || !launch_fits(B, kPruneThreads)) return ASV_EINVAL;
   if (B == 0) return ASV_OK;
   if (!tree || !parent || !draft_tok || !req_offsets || !req_status) return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -497,7 +500,7 @@ extern "C" int asv_draft_prune(const asv_draft_tree* tree, int32_t B, const int3
 extern "C" int asv_tree_meta(const int32_t* parent, const int32_t* req_offsets, int32_t B,
                              int32_t N, const int32_t* pos_base, int32_t mask_words,
                              int32_t* pos, uint32_t* mask, int32_t* req_status, void* stream) {
-  if (B < 0 || N < B || (B == 0) != (N == 0)) return ASV_EINVAL;
+  if (B < 0 || N < B || (B == 0) != (N == 0) || !launch_fits(B, kMetaThreads)) return ASV_EINVAL;
   if (B == 0) return ASV_OK;
   if (!parent || !req_offsets || !req_status || (mask && mask_words < 1)) return ASV_EINVAL;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
@@ -508,7 +511,9 @@ extern "C" int asv_tree_meta(const int32_t* parent, const int32_t* req_offsets, 
 }
 
 extern "C" int asv_commit(const asv_commit_args* a, void* stream) {
-  if (!a || a->B < 0 || a->N < a->B || (a->B == 0) != (a->N == 0)) return ASV_EINVAL;
+  if (!a || a->B < 0 || a->N < a->B || (a->B == 0) != (a->N == 0) ||
+      !launch_fits(a->B, kCommitThreads))
+    return ASV_EINVAL;
   if (a->B == 0) return ASV_OK;
   if (!a->req_offsets || !a->draft_tok || !a->accepted_len || !a->accepted_path ||
       !a->bonus_token || !a->commit_off || !a->commit_tok || !a->commit_row || !a->req_status)

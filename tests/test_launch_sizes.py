@@ -62,3 +62,25 @@ def test_verify(lib, layout):
     V = 3 << 23                            # 98304 slabs x 256 row tiles of 256 rows, two launches at most
     if layout != _abi.W_FP8:
         assert call(1, 65535, V, True) == asv.ASV_EINVAL
+
+
+def test_around_the_step(lib):
+    B = 1 << 24
+    status = lib.asv_draft_prune(BIG, B, None, 5, 2 * BIG, 3 * BIG, 4 * BIG, 5 * BIG, None)
+    assert status == asv.ASV_EINVAL
+    assert lib.asv_tree_meta(BIG, 2 * BIG, B, B, None, 0, 3 * BIG, None, 4 * BIG, None) == asv.ASV_EINVAL
+    c = _abi.AsvCommitArgs()
+    c.B = c.N = B
+    for i, f in enumerate(("req_offsets", "draft_tok", "accepted_len", "accepted_path", "bonus_token",
+                           "commit_off", "commit_tok", "commit_row", "req_status")):
+        setattr(c, f, (i + 1) * BIG)
+    assert lib.asv_commit(ctypes.byref(c), None) == asv.ASV_EINVAL
+
+
+def test_draft_step(lib):
+    d = _abi.AsvDraftArgs()
+    d.B, d.H, d.V = 1 << 17, 64, 1 << 24         # 2^17 slabs x 2^11 row tiles of 128 ids x 256 rows
+    for i, f in enumerate(("hidden", "w_draft", "tree", "topk_id", "topk_logp", "row_lse", "front_tok")):
+        setattr(d, f, (i + 1) * BIG)
+    d.shape = (ctypes.c_int32 * 3)(1, 1, 1)
+    assert lib.asv_draft_step(ctypes.byref(d), 80 * BIG, 1 << 60, None) == asv.ASV_EINVAL
