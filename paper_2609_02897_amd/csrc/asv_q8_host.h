@@ -14,7 +14,7 @@ namespace {
 using Q8Ids64 = Q8Family<64, 64, 4, false>;
 using Q8Ids128 = Q8Family<128, 64, 3, false>;
 using Q8Ids256 = Q8Family<256, 64, 2, false>;
-// Beyond: tiles of 256 ids, and what the tail of a launch runs.
+// Beyond: tiles of 256 ids, and what the tail of a launch runs (of 128 rows; of 256 where it is alone).
 template <int TR> using Q8Rows = Q8Family<256, TR, 3, true>;
 template <int TR, int IDS> using Q8Tail = Q8Family<IDS, TR, TR == 256 ? 2 : 3, false>;
 

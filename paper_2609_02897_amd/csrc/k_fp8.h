@@ -9,10 +9,10 @@
 //
 // The products run on the bf16 matrix instructions: a code has four significant bits and its scale is a
 // power of two, so bf16 holds its value exactly, and the sums are fp32 sums. The 8-bit matrix
-// instructions (v_mfma_f32_16x16x128_f8f6f4, v_mfma_f32_16x16x32_fp8_fp8) are not used: they
-// align the products of one instruction to the largest and keep about 13 bits below it (measured: errors
-// up to 2^-12 of the largest product, logits 1.5e-5 off in the 2-norm against 1e-7), which would turn the
-// top-1 of rows with close logits.
+// instructions (v_mfma_f32_16x16x128_f8f6f4, v_mfma_f32_16x16x32_fp8_fp8) are not used, as what they give are
+// not fp32 sums: they align the products of one instruction to the largest and keep 9 to 13 bits below it
+// (128 normal values: errors up to 2^-13 of the largest product, 1.5e-5 in the 2-norm against the 1e-7 of
+// these kernels; values over twelve binades: 6.4e-5).
 //
 // What 8 bits buy is the weight's stream, which bounds the product up to a few hundred rows: W
 // goes to LDS as codes, half of K1's bytes, and each fragment is widened in registers by
